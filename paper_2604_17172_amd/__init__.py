@@ -10,6 +10,9 @@ not been built.
 Convenience wrappers (``compress``, ``decompress``, ``reduce_fused``,
 ``compress_chunked``) allocate outputs and workspaces with torch and call
 the C ABI on ``torch.cuda.current_stream()``.
+
+The paged 8-bit key/value cache (``KVCache``, ``kv_plan``, ``kv_store``,
+``kv_attend``) is in ``kv.py``, its kernels in ``csrc/kv_*.hip``.
 """
 from __future__ import annotations
 
@@ -434,3 +437,8 @@ def compress_chunked_table(x: torch.Tensor, block_bytes: int, chunk_bytes: int, 
                                        sizes.data_ptr(), flags.data_ptr(), epoch, ws.data_ptr(), ws.numel(),
                                        _stream(stream)), "uzip_compress_chunked_table")
     return out, slot, sizes, flags
+
+
+from .kv import (KV_MAX_REQUESTS, KV_MAX_ROWS, KVCache, KVPlan, kv_attend, kv_attend_workspace,  # noqa: E402,F401
+                 kv_plan, kv_plan_buffers, kv_store, uzip_kv_attend, uzip_kv_attend_workspace, uzip_kv_cache,
+                 uzip_kv_max_runs, uzip_kv_plan, uzip_kv_store)

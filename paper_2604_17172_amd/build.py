@@ -5,15 +5,20 @@
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = os.path.join(HERE, "csrc", "uzip.hip")
+CSRC = os.path.join(HERE, "csrc")
+SRC = os.path.join(CSRC, "uzip.hip")
+SOURCES = [SRC, os.path.join(CSRC, "kv_cache.hip"), os.path.join(CSRC, "kv_attend.hip")]
 LIB_PATH = os.path.join(HERE, "_build", "libuzip.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # no packed fp32 instructions in any kernel
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # the fused reduce is an exact fixed-order binary32 sum
@@ -22,15 +27,28 @@ HIPCC_FLAGS = [
 ]
 
 
-def build(verbose: bool = False) -> str:
-    os.makedirs(os.path.dirname(LIB_PATH), exist_ok=True)
-    tmp = LIB_PATH + ".tmp"
-    cmd = ["hipcc", *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), SRC, "-o", tmp]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+def _hipcc(args: list[str], verbose: bool) -> None:
+    res = subprocess.run(["hipcc", *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), *args], capture_output=True,
+                         text=True)
     if res.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
     if verbose and res.stderr:
         print(res.stderr)
+
+
+def build(verbose: bool = False) -> str:
+    """Compile every source, side by side, and link the library."""
+    os.makedirs(os.path.dirname(LIB_PATH), exist_ok=True)
+    objs = tempfile.mkdtemp(prefix="uzip_build_")
+    try:
+        units = [(src, os.path.join(objs, os.path.basename(src) + ".o")) for src in SOURCES]
+        with ThreadPoolExecutor(max_workers=8) as pool:
+            for job in [pool.submit(_hipcc, ["-c", src, "-o", obj], verbose) for src, obj in units]:
+                job.result()
+        tmp = LIB_PATH + ".tmp"
+        _hipcc(["-shared", *[obj for _, obj in units], "-o", tmp], verbose)
+    finally:
+        shutil.rmtree(objs, ignore_errors=True)
     os.replace(tmp, LIB_PATH)
     return LIB_PATH
 
