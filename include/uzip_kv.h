@@ -60,6 +60,7 @@ typedef struct {
 /* Requests of one plan, and rows of one call. */
 #define UZIP_KV_MAX_REQUESTS 4096
 #define UZIP_KV_MAX_ROWS (1u << 22)
+#define UZIP_KV_MAX_ROW_HEADS (1u << 27) /* rows times query heads of one uzip_kv_attend */
 
 /* Entries of d_runs: the most runs that n_rows new tokens of n_reqs requests
  * can make, at least 1.  Returns 0 for invalid arguments. */
@@ -135,7 +136,8 @@ size_t uzip_kv_attend_workspace(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_
  *   d_out:       row r, head a at d_out + r * out_row + a * out_head (elements).
  *   d_lse:       [n_rows][n_q_heads] (may be NULL).
  *   d_ws, ws_bytes: at least uzip_kv_attend_workspace.
- * n_q_heads is a multiple of n_heads.  n_reqs <= UZIP_KV_MAX_REQUESTS.
+ * n_q_heads is a multiple of n_heads <= 1024; n_rows * n_q_heads <=
+ * UZIP_KV_MAX_ROW_HEADS; n_reqs <= UZIP_KV_MAX_REQUESTS.
  * Errors: EINVAL, ENOSPC, EHIP, EUNSUPPORTED. */
 uzip_status uzip_kv_attend(const uzip_kv_cache *cache, uzip_dtype dtype, const void *d_q, int64_t q_row,
                            int64_t q_head, uint32_t n_rows, uint32_t n_q_heads, const int32_t *d_table,

@@ -14,7 +14,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SRC = os.path.join(CSRC, "uzip.hip")
-SOURCES = [SRC, os.path.join(CSRC, "kv_cache.hip"), os.path.join(CSRC, "kv_attend.hip")]
+SOURCES = [SRC] + [os.path.join(CSRC, name) for name in (
+    "kv_cache.hip", "kv_attend.hip", *(f"kv_attend_{dim}.hip" for dim in (64, 96, 128, 192, 256)))]
 LIB_PATH = os.path.join(HERE, "_build", "libuzip.so")
 
 HIPCC_FLAGS = [
