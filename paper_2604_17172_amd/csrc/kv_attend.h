@@ -29,7 +29,8 @@ struct AttendArgs {
   float *part_ml;    // [slot][row of the block][2]: their m and l
   uint32_t n_rows, n_q_heads, group, max_pages, n_reqs, window;
   uint32_t target;   // pieces that fill the GPU
-  float scale_log2;  // scale * log2 e
+  float scale_log2;  // |scale| log2 e
+  bool negate;       // scale < 0: the queries change sign instead
   bool q_vec, out_vec;  // rows start at multiples of 16 (q) and 4 elements (out), so loads and stores may be wide
 };
 
@@ -70,6 +71,18 @@ __device__ __forceinline__ void seen_range(const AttendArgs &a, const Request &q
   *hi = min(max(p1 + 1, 0), q.len);
   *lo = a.window && (int64_t)p0 + 1 > a.window ? (int32_t)((int64_t)p0 + 1 - a.window) : 0;
 }
+
+// The tokens that the row at a place sees: first .. first + span.
+struct Seen {
+  int32_t first;
+  uint32_t span;
+};
+__device__ __forceinline__ Seen seen_by(const AttendArgs &a, int32_t place) {
+  if (place < 0) return {INT32_MAX, 0};  // none: no token is that far
+  const int32_t first = a.window && (int64_t)place + 1 > a.window ? (int32_t)((int64_t)place + 1 - a.window) : 0;
+  return {first, (uint32_t)(place - first)};
+}
+__device__ __forceinline__ bool sees(const Seen &s, int32_t t) { return (uint32_t)t - (uint32_t)s.first <= s.span; }
 
 struct Piece {
   Request q;
@@ -186,6 +199,12 @@ struct Query<UZIP_FP32> {  // 24 bits: three bf16 terms each
   static constexpr int kTerms = 3, kProbs = 3;
 };
 
+// Infinities (e5m2 has them) times the second and third term of a probability,
+// which may be 0 or negative, are no infinities: there they are always left out of
+// the product and added after it.
+template <int T, int CODE>
+constexpr bool kLeaveOut = CODE == UZIP_E5M2 && Query<T>::kProbs > 1;
+
 union Frag {
   bf16x8 b;
   f16x8 h;
@@ -243,10 +262,10 @@ __device__ __forceinline__ f32x4 score_mfma(const Frag &k, const Frag *q, f32x4 
   return c;
 }
 
-// Eight values as the query's fragments: fp32 in three bf16 terms, each the
+// Eight values, or their negatives, as the query's fragments: fp32 in three bf16 terms, each the
 // rounding of what the ones before left.
 template <int T>
-__device__ __forceinline__ void query_frag(const typename Elem<T>::type *x, bool wide, Frag *f) {
+__device__ __forceinline__ void query_frag(const typename Elem<T>::type *x, bool wide, bool negate, Frag *f) {
   if constexpr (T == UZIP_FP32) {
     float v[8];
     if (wide) {
@@ -272,6 +291,10 @@ __device__ __forceinline__ void query_frag(const typename Elem<T>::type *x, bool
       else f[0].b[j] = x[j];
     }
   }
+  if (negate) {
+#pragma unroll
+    for (int i = 0; i < Query<T>::kTerms; ++i) f[i].u = uint4{f[i].u.x ^ 0x80008000u, f[i].u.y ^ 0x80008000u, f[i].u.z ^ 0x80008000u, f[i].u.w ^ 0x80008000u};
+  }
 }
 
 // Words of eight codes that are NaN or infinite; the sign bits say where.
@@ -287,6 +310,50 @@ __device__ __forceinline__ uint32_t keep_tokens(uint32_t w, int32_t t, int32_t l
   const uint32_t low = below == 4 ? 0xFFFFFFFFu : (1u << (8 * below)) - 1u;
   return w & high & ~low;
 }
+
+// Four results next to each other.
+template <int T>
+__device__ __forceinline__ void store4(typename Elem<T>::type *out, f32x4 x, bool wide) {
+  typedef typename Elem<T>::type Value;
+  Value o[4] __attribute__((aligned(16)));
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = (Value)x[j];
+  if (wide) {
+    if constexpr (sizeof(Value) == 2) *(uint2 *)out = *(uint2 *)o;
+    else *(uint4 *)out = *(uint4 *)o;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out[j] = o[j];
+  }
+}
+
+// Zero for codes that are NaN or infinite.
+template <int CODE>
+__device__ __forceinline__ uint32_t bounded(uint32_t w) {
+  return w & ~((unbounded<CODE>(w) >> 7) * 0xFFu);
+}
+template <int CODE>
+__device__ __forceinline__ bool any_unbounded(uint4 w) {
+  return (unbounded<CODE>(w.x) | unbounded<CODE>(w.y) | unbounded<CODE>(w.z) | unbounded<CODE>(w.w)) != 0;
+}
+template <int CODE>
+__device__ __forceinline__ uint4 bounded(uint4 w) {
+  return uint4{bounded<CODE>(w.x), bounded<CODE>(w.y), bounded<CODE>(w.z), bounded<CODE>(w.w)};
+}
+
+// 1 for each of the eight codes that is NaN (kind 0), infinite (1) or minus
+// infinite (2), 0 for the others, as a fragment.
+template <int CODE>
+__device__ __forceinline__ Frag class_frag(uint32_t lo, uint32_t hi, int kind) {
+  Frag f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float x = decode<CODE>(((j < 4 ? lo : hi) >> (8 * (j % 4))) & 0xFFu);
+    f.b[j] = (__bf16)((kind == 0 ? x != x : x == (kind == 1 ? INFINITY : -INFINITY)) ? 1.0f : 0.0f);
+  }
+  return f;
+}
+__device__ __forceinline__ float class_value(int kind) { return kind == 0 ? NAN : kind == 1 ? INFINITY : -INFINITY; }
 
 // ------------------------------------------------------------------ few rows
 // One workgroup for up to 16 NM rows and a piece of their tokens, one wave a
@@ -322,22 +389,26 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
 
   // the rows' queries and places
   Frag q[NM][F::kKeySteps][TERMS];
-  int32_t place[NM];
+  Seen seen[NM];
 #pragma unroll
   for (int n = 0; n < NM; ++n) {
     const uint32_t r = r0 + 16 * n + col;
     const bool here = r < list;
     const uint32_t tok = here ? r / a.group : 0, head = pc.head * a.group + (here ? r % a.group : 0);
-    place[n] = here ? pc.q.base + (int32_t)tok : -1;
+    seen[n] = seen_by(a, here ? pc.q.base + (int32_t)tok : -1);
     const Value *x = (const Value *)a.q + (int64_t)(pc.q.first + (int32_t)tok) * a.q_row + (int64_t)head * a.q_head;
 #pragma unroll
     for (int s = 0; s < F::kKeySteps; ++s) {
       const uint32_t d = s < 2 * F::kPairs ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
-      query_frag<T>(x + d, a.q_vec, q[n][s]);
+      query_frag<T>(x + d, a.q_vec, a.negate, q[n][s]);
     }
   }
   // the first and the last place of the block's rows
   const int32_t p_min = pc.q.base + (int32_t)(r0 / a.group), p_max = pc.q.base + (int32_t)((min(list, r0 + F::kRows) - 1) / a.group);
+
+  auto all_see = [&](int32_t t0) {
+    return t0 + kStep - 1 <= p_min && (a.window == 0 || (int64_t)t0 > (int64_t)p_max - a.window);
+  };
 
   f32x4 acc[NM][F::kChannels];
   float m[NM], l[NM];
@@ -381,6 +452,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
 
   uint32_t step = begin + wave;
   int32_t key_page = -1, value_page = -1;
+  bool odd = false;  // a NaN or an infinity was left out
   if (step < end) {
     const int32_t t0 = (int32_t)(step * kStep);
     key_page = page_of(t0 + key_chunk);
@@ -418,23 +490,19 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
     if (more) load_keys(t_next, key_page);
 
     // scores, and what is not seen
-    const bool whole = t0 >= lo && t0 + kStep - 1 <= p_min && (a.window == 0 || (int64_t)t0 > (int64_t)p_max - a.window) &&
-                       __all(page_ok);
+    const bool whole = all_see(t0) && __all(page_ok);
     const int32_t t_lane = t0 + value_chunk;
+    float c = ks_scale;  // what a score is still to be multiplied by
+    if (!whole) {
 #pragma unroll
-    for (int n = 0; n < NM; ++n)
+      for (int n = 0; n < NM; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float x = s[n][i][j] * ks_scale;
-          if (!whole) {
-            const int32_t t = t_lane + 4 * i + j;
-            const bool seen = page_ok && t <= place[n] && (a.window == 0 || (int64_t)t > (int64_t)place[n] - a.window);
-            x = seen ? x : -INFINITY;
-          }
-          s[n][i][j] = x;
-        }
+          for (int j = 0; j < 4; ++j)
+            s[n][i][j] = page_ok && sees(seen[n], t_lane + 4 * i + j) ? s[n][i][j] * c : -INFINITY;
+      c = 1;
+    }
 
     // The maximum is taken anew only where a score passes the old one by more
     // than 8: powers of two up to 2^8 cost no precision, and most steps need
@@ -447,6 +515,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) top = fmaxf(top, s[n][i][j]);
+      top *= c;
       if (__any(top > m[n] + 8.0f)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -462,7 +531,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          float x = exp2_fast(s[n][i][j] - base);
+          float x = exp2_fast(__builtin_fmaf(s[n][i][j], c, -base));
           l[n] += x;
 #pragma unroll
           for (int t = 0; t < PROBS; ++t) {
@@ -472,54 +541,23 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
         }
     }
 
-    // Codes that no row sees count as zero: 0 times NaN would not.  A NaN or an
-    // infinity that some rows see and others do not is taken out of the product
-    // and added to the rows that see it.
-    if (!whole) {
-      bool odd = false;
+    // Codes that no row sees count as zero, for 0 times NaN is not 0.  A NaN or an
+    // infinity that some rows see and others do not is left for after the loop.
+    if (!whole || kLeaveOut<T, CODE>) {
 #pragma unroll
       for (int c = 0; c < F::kChannels; ++c) {
-        uint32_t *w = (uint32_t *)&v16[c];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[i] = page_ok ? keep_tokens(w[i], t_lane + 4 * i, lo, hi) : 0u;
-          odd = odd || unbounded<CODE>(w[i]) != 0;
+        uint4 w = v16[c];
+        if (!whole) {
+          w.x = page_ok ? keep_tokens(w.x, t_lane, lo, hi) : 0u;
+          w.y = page_ok ? keep_tokens(w.y, t_lane + 4, lo, hi) : 0u;
+          w.z = page_ok ? keep_tokens(w.z, t_lane + 8, lo, hi) : 0u;
+          w.w = page_ok ? keep_tokens(w.w, t_lane + 12, lo, hi) : 0u;
         }
-      }
-      if (p_min != p_max && __any(odd)) {
-#pragma unroll
-        for (int c = 0; c < F::kChannels; ++c) {
-          uint32_t *w = (uint32_t *)&v16[c];
-#pragma unroll 1
-          for (int kind = 0; kind < 3; ++kind) {  // NaN, infinity, -infinity
-            const float value = kind == 0 ? NAN : kind == 1 ? INFINITY : -INFINITY;
-#pragma unroll
-            for (int n = 0; n < NM; ++n) {
-              f32x4 hits = {0, 0, 0, 0};
-#pragma unroll
-              for (int u = 0; u < 2; ++u) {
-                Frag is, see;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const uint32_t code = (w[2 * u + j / 4] >> (8 * (j % 4))) & 0xFFu;
-                  const float x = decode<CODE>(code);
-                  is.b[j] = (__bf16)((kind == 0 ? x != x : x == value) ? 1.0f : 0.0f);
-                  const int32_t t = t_lane + 8 * u + j;
-                  see.b[j] = (__bf16)(page_ok && t <= place[n] && (a.window == 0 || (int64_t)t > (int64_t)place[n] - a.window) ? 1.0f : 0.0f);
-                }
-                hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is.b, see.b, hits, 0, 0, 0);
-              }
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (hits[j] > 0) acc[n][c][j] += value;
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t bad = unbounded<CODE>(w[i]) >> 7;
-            w[i] &= ~(bad * 0xFFu);
-          }
+        if (p_min != p_max || kLeaveOut<T, CODE>) {
+          odd = odd || any_unbounded<CODE>(w);
+          w = bounded<CODE>(w);
         }
+        v16[c] = w;
       }
     }
 
@@ -541,6 +579,36 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
       if (step + 2 * F::kWaves < end) {
         key_page = page_of(t_next + F::kWaves * kStep + key_chunk);
         value_page = page_of(t_next + F::kWaves * kStep + value_chunk);
+      }
+    }
+  }
+
+  if (__any(odd)) {  // the rows that see such a value get it
+#pragma unroll 1
+    for (step = begin + wave; step < end; step += F::kWaves) {
+      const int32_t t0 = (int32_t)(step * kStep), t_lane = t0 + value_chunk;
+      if (all_see(t0) && !kLeaveOut<T, CODE>) continue;
+      load_values(t0, page_of(t_lane));
+#pragma unroll
+      for (int c = 0; c < F::kChannels; ++c) {
+        if (!__any(any_unbounded<CODE>(v16[c]))) continue;
+#pragma unroll 1
+        for (int kind = 0; kind < 3; ++kind)
+#pragma unroll
+          for (int n = 0; n < NM; ++n) {
+            f32x4 hits = {0, 0, 0, 0};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              Frag see;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) see.b[j] = (__bf16)(page_here && sees(seen[n], t_lane + 8 * u + j) ? 1.0f : 0.0f);
+              const Frag is = u ? class_frag<CODE>(v16[c].z, v16[c].w, kind) : class_frag<CODE>(v16[c].x, v16[c].y, kind);
+              hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is.b, see.b, hits, 0, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (hits[j] > 0) acc[n][c][j] += class_value(kind);
+          }
       }
     }
   }
@@ -606,50 +674,351 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
     Value *out = (Value *)a.out + row * a.out_row + head * a.out_head;
     const float inv = l[n] == 0 ? 0.0f : 1.0f / l[n];
 #pragma unroll
-    for (int c = 0; c < F::kChannels; ++c) {
-      Value o[4] __attribute__((aligned(4 * sizeof(Value))));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = (Value)(acc[n][c][j] * inv);
-      if (a.out_vec) {
-        if constexpr (sizeof(Value) == 2) *(uint2 *)(out + 16 * c + 4 * g) = *(uint2 *)o;
-        else *(uint4 *)(out + 16 * c + 4 * g) = *(uint4 *)o;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) out[16 * c + 4 * g + j] = o[j];
-      }
-    }
+    for (int c = 0; c < F::kChannels; ++c) store4<T>(out + 16 * c + 4 * g, acc[n][c] * inv, a.out_vec);
     if (a.lse && g == 0) a.lse[row * a.n_q_heads + head] = l[n] == 0 ? -INFINITY : (m[n] + log2_fast(l[n])) * 0.6931471805599453f;
   }
 }
 
-// ------------------------------------------------------------------ joining pieces
-// One workgroup for each block that was split: the pieces' maxima, sums and accs.
-template <int T, int D>
-__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, uint32_t rows, int64_t least, int64_t most) {
-  typedef typename Elem<T>::type Value;
-  Piece pc;
-  if (!find_piece<256, true>(a, rows, least, most, blockIdx.x, &pc)) return;
-  const uint32_t list = (uint32_t)pc.q.rows * a.group, r0 = pc.block * rows, n = min(rows, list - r0);
-  constexpr uint32_t kLanes = D / 4;  // lanes of a row, four channels each
-  for (uint32_t i = threadIdx.x; i < n * kLanes; i += 256) {
-    const uint32_t in = i / kLanes, d = 4 * (i % kLanes), r = r0 + in;
-    float m = -INFINITY;
-    for (uint32_t s = 0; s < pc.splits; ++s) m = fmaxf(m, a.part_ml[2 * ((size_t)(pc.slot + s) * rows + in)]);
-    f32x4 acc = {0, 0, 0, 0};
-    float l = 0;
-    for (uint32_t s = 0; s < pc.splits; ++s) {
-      const size_t at = (size_t)(pc.slot + s) * rows + in;
-      const float ms = a.part_ml[2 * at], w = ms == m ? 1.0f : exp2_fast(ms - m);
-      l += w * a.part_ml[2 * at + 1];
-      acc += w * *(const f32x4 *)(a.part_acc + at * D + d);
-    }
-    const int64_t row = pc.q.first + (int64_t)(r / a.group), head = (int64_t)pc.head * a.group + r % a.group;
-    Value *out = (Value *)a.out + row * a.out_row + head * a.out_head + d;
-    const float inv = l == 0 ? 0.0f : 1.0f / l;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) out[j] = (Value)(acc[j] * inv);
-    if (a.lse && d == 0) a.lse[row * a.n_q_heads + head] = l == 0 ? -INFINITY : (m + log2_fast(l)) * 0.6931471805599453f;
+// ------------------------------------------------------------------ many rows
+// One workgroup for 128 rows and a piece of their tokens, a wave 32 rows: the
+// step's codes are staged in LDS and every wave reads them all.  As above, S^T = K
+// Q^T and O^T = V^T P^T in matrix instructions of 32 x 32 x 16 (a lane holds, of the
+// result, rows 8 (i / 4) + 4 (lane / 32) + i % 4 of column lane % 32): row m = 8 a + 4
+// b + c of a tile of 32 keys is its token 16 b + 4 a + c, so a lane's 16 scores are of
+// 16 tokens in a row and are its part of the second product's operand.
+//
+// LDS holds codes, not bf16: half the bytes to read, for one conversion per two
+// codes and wave.  16-byte chunks are placed so that eight lanes next to each other
+// read eight different places of 128 bytes.
+template <int D>
+struct ManyRows {
+  static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves;
+  static constexpr int kChunks = D / 16;              // of a key, and blocks of 16 channels
+  static constexpr int kAll = kStep * kChunks, kLoads = (kAll + kThreads - 1) / kThreads;  // chunks of keys; of each thread; as many of values
+  __device__ static __forceinline__ bool has(uint32_t n) { return kAll % kThreads == 0 || n < kAll; }
+  // Chunk c of token t of a step, and chunk c (16 tokens) of channel d, in units of 16 bytes.
+  __device__ static __forceinline__ uint32_t key_at(uint32_t t, uint32_t c) {
+    uint32_t turn;
+    if constexpr (kChunks % 8 == 0) turn = (t & 3) | ((t >> 4) & 1) << 2;
+    else if constexpr (kChunks % 4 == 0) turn = ((t >> 1) & 1) | ((t >> 4) & 1) << 1;
+    else turn = (t >> 4) & 1;
+    return t * kChunks + (c ^ turn);
   }
+  __device__ static __forceinline__ uint32_t value_at(uint32_t d, uint32_t c) { return 4 * d + (c ^ ((d >> 1) & 3)); }
+};
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int T>
+__device__ __forceinline__ f32x16 score_mfma32(const Frag &k, const Frag &q, f32x16 c) {
+  if constexpr (T == UZIP_FP16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(k.h, q.h, c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.b, q.b, c, 0, 0, 0);
+}
+
+template <int T, int CODE, int D>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_many_kernel(AttendArgs a, int64_t least, int64_t most) {
+  typedef ManyRows<D> F;
+  typedef typename Elem<T>::type Value;
+  constexpr int PROBS = Query<T>::kProbs, kTiles = kStep / 32, kChannels = D / 32, kKeySteps = D / 16;
+  __shared__ uint4 keys[2][F::kAll];
+  __shared__ uint4 values[2][F::kAll];
+  __shared__ float key_scale[2][4], value_scale[2][4];  // of 16 tokens each; a key's is -1 where there is no page
+  __shared__ uint32_t odd;                              // a NaN or an infinity was left out
+  Piece pc;
+  if (!find_piece<F::kThreads, false>(a, F::kRows, least, most, blockIdx.x, &pc)) return;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+  const uint32_t list = (uint32_t)pc.q.rows * a.group, P = a.c.page;
+  // the blocks with the most tokens first: the last ones to run are short
+  const uint32_t r0 = ((list + F::kRows - 1) / F::kRows - 1 - pc.block) * F::kRows;
+  int32_t lo, hi;
+  seen_range(a, pc.q, r0, min(list, r0 + F::kRows), &lo, &hi);
+  const uint32_t step0 = (uint32_t)lo / kStep, steps = hi > lo ? ((uint32_t)hi + kStep - 1) / kStep - step0 : 0;
+  const uint32_t share = (steps + pc.splits - 1) / pc.splits;
+  const uint32_t begin = step0 + min(steps, pc.split * share), end = step0 + min(steps, (pc.split + 1) * share);
+
+  // this wave's rows
+  const uint32_t w0 = r0 + 32 * wave, r = w0 + col;
+  const bool here = r < list;
+  const uint32_t tok = here ? r / a.group : 0, head = pc.head * a.group + (here ? r % a.group : 0);
+  const Seen seen = seen_by(a, here ? pc.q.base + (int32_t)tok : -1);
+  const uint32_t w1 = min(list, w0 + 32);
+  const int32_t p_min = w0 < list ? pc.q.base + (int32_t)(w0 / a.group) : -1;
+  const int32_t p_max = w0 < list ? pc.q.base + (int32_t)((w1 - 1) / a.group) : -1;
+  Frag q[kKeySteps];
+  {
+    const Value *x = (const Value *)a.q + (int64_t)(pc.q.first + (int32_t)tok) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int s = 0; s < kKeySteps; ++s) query_frag<T>(x + 32 * (s / 2) + 16 * half + 8 * (s % 2), a.q_vec, a.negate, &q[s]);
+  }
+  f32x16 acc[kChannels];
+#pragma unroll
+  for (int c = 0; c < kChannels; ++c) acc[c] = f32x16{};
+  float m = -INFINITY, l = 0;
+
+  // staging: thread's chunks n = tid + 256 i
+  const int32_t *table = a.table + (size_t)pc.req * a.max_pages;
+  const size_t page_bytes = (size_t)P * D;
+  uint4 stage_k[F::kLoads], stage_v[F::kLoads];
+  float stage_scale = 0;
+  const int32_t b_min = pc.q.base + (int32_t)(r0 / a.group), b_max = pc.q.base + (int32_t)((min(list, r0 + F::kRows) - 1) / a.group);
+  auto all_see = [&](int32_t t0) {  // all rows of the block
+    return t0 + kStep - 1 <= b_min && (a.window == 0 || (int64_t)t0 > (int64_t)b_max - a.window);
+  };
+  auto page_of = [&](int32_t t) { return t < hi ? table[(uint32_t)t >> a.c.page_shift] : -1; };
+  auto load = [&](uint32_t step) {
+    const int32_t t0 = (int32_t)(step * kStep);
+    const bool edge = !all_see(t0);
+#pragma unroll
+    for (int i = 0; i < F::kLoads; ++i) {
+      const uint32_t n = tid + F::kThreads * i, t = n / F::kChunks, c = n % F::kChunks;
+      if (!F::has(n)) break;
+      int32_t page = page_of(t0 + (int32_t)(t & ~15u));
+      page = (uint32_t)page < a.c.n_pages ? page : 0;
+      stage_k[i] = *(const uint4 *)(a.c.k + ((size_t)page * a.c.heads + pc.head) * page_bytes +
+                                    (((uint32_t)t0 + t) & (P - 1)) * D + 16 * c);
+    }
+#pragma unroll
+    for (int i = 0; i < F::kLoads; ++i) {
+      const uint32_t n = tid + F::kThreads * i, d = n / 4, c = n % 4;
+      if (!F::has(n)) break;
+      const int32_t t = t0 + 16 * (int32_t)c, page = page_of(t);
+      const bool ok = (uint32_t)page < a.c.n_pages;
+      uint4 w = *(const uint4 *)(a.c.v + ((size_t)(ok ? page : 0) * a.c.heads + pc.head) * page_bytes + (size_t)d * P +
+                                 ((uint32_t)t & (P - 1)));
+      if (!ok) w = uint4{0, 0, 0, 0};
+      if (edge) {  // codes that no row sees count as zero, for 0 times NaN is not 0
+        w.x = keep_tokens(w.x, t, lo, hi);
+        w.y = keep_tokens(w.y, t + 4, lo, hi);
+        w.z = keep_tokens(w.z, t + 8, lo, hi);
+        w.w = keep_tokens(w.w, t + 12, lo, hi);
+      }
+      if (edge || kLeaveOut<T, CODE>) {
+        if (any_unbounded<CODE>(w)) {  // seen by some rows perhaps: left for after the loop
+          odd = 1;
+          w = bounded<CODE>(w);
+        }
+      }
+      stage_v[i] = w;
+    }
+    if (tid < 8) {
+      const int32_t page = page_of(t0 + 16 * (int32_t)(tid & 3));
+      const bool ok = (uint32_t)page < a.c.n_pages;
+      const size_t ph = (size_t)(ok ? page : 0) * a.c.heads + pc.head;
+      const float s = pow2((tid < 4 ? a.c.k_exp : a.c.v_exp)[ph]);
+      stage_scale = ok ? s : tid < 4 ? -1.0f : 1.0f;
+    }
+  };
+  auto put = [&](uint32_t step) {
+    const uint32_t b = step & 1;
+#pragma unroll
+    for (int i = 0; i < F::kLoads; ++i) {
+      const uint32_t n = tid + F::kThreads * i;
+      if (!F::has(n)) break;
+      keys[b][F::key_at(n / F::kChunks, n % F::kChunks)] = stage_k[i];
+      values[b][F::value_at(n / 4, n % 4)] = stage_v[i];
+    }
+    if (tid < 4) key_scale[b][tid] = stage_scale;
+    else if (tid < 8) value_scale[b][tid - 4] = stage_scale;
+  };
+  if (tid == 0) odd = 0;
+  __syncthreads();
+  if (begin < end) {
+    load(begin);
+    put(begin);
+  }
+  __syncthreads();
+  const uint32_t key_row = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);  // token of this lane's row
+  for (uint32_t step = begin; step < end; ++step) {
+    const uint32_t b = step & 1;
+    const int32_t t0 = (int32_t)(step * kStep);
+    if (step + 1 < end) load(step + 1);
+    if (w0 < list && t0 <= p_max && (a.window == 0 || (int64_t)t0 + kStep - 1 > (int64_t)p_min - a.window)) {
+      f32x16 s[kTiles];
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        s[i] = f32x16{};
+#pragma unroll
+        for (int c = 0; c < kChannels; ++c) {
+          const uint4 w = keys[b][F::key_at(32 * i + key_row, 2 * c + half)];
+          s[i] = score_mfma32<T>(key_frag<T, CODE>(w.x, w.y), q[2 * c], s[i]);
+          s[i] = score_mfma32<T>(key_frag<T, CODE>(w.z, w.w), q[2 * c + 1], s[i]);
+        }
+      }
+      float ks[kTiles], vs[kTiles];  // ks: what a score is still to be multiplied by
+      bool page_ok[kTiles], pages_ok = true;
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        const float x = key_scale[b][2 * i + half];
+        page_ok[i] = x >= 0;
+        pages_ok = pages_ok && page_ok[i];
+        ks[i] = x * a.scale_log2;
+        vs[i] = value_scale[b][2 * i + half];
+      }
+      const bool whole = t0 + kStep - 1 <= p_min && (a.window == 0 || (int64_t)t0 > (int64_t)p_max - a.window) && __all(pages_ok);
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            s[i][j] = page_ok[i] && sees(seen, t0 + 32 * i + 16 * (int32_t)half + j) ? s[i][j] * ks[i] : -INFINITY;
+          ks[i] = 1;
+        }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        float t = s[i][0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) t = fmaxf(t, s[i][j]);
+        top = fmaxf(top, t * ks[i]);
+      }
+      if (__any(top > m + 8.0f)) {
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m2 = fmaxf(m, top);
+        const float shrink = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
+        m = m2;
+        l *= shrink;
+#pragma unroll
+        for (int c = 0; c < kChannels; ++c) acc[c] *= shrink;
+      }
+      const float base = m == -INFINITY ? 0.0f : m;
+      Frag p[kTiles][2][PROBS];
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          float x = exp2_fast(__builtin_fmaf(s[i][j], ks[i], -base));
+          l += x;
+#pragma unroll
+          for (int t = 0; t < PROBS; ++t) {
+            p[i][j / 8][t].b[j % 8] = (__bf16)x;
+            if (t + 1 < PROBS) x -= (float)p[i][j / 8][t].b[j % 8];
+          }
+        }
+#pragma unroll
+      for (int c = 0; c < kChannels; ++c)
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          const uint4 w = values[b][F::value_at(32 * c + col, 2 * i + half)];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const Frag v = u ? codes_bf16<CODE>(w.z, w.w, vs[i]) : codes_bf16<CODE>(w.x, w.y, vs[i]);
+#pragma unroll
+            for (int t = PROBS - 1; t >= 0; --t)
+              acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.b, p[i][u][t].b, acc[c], 0, 0, 0);
+          }
+        }
+    }
+    // the other buffer was last read in the step before, which every wave has left
+    if (step + 1 < end) put(step + 1);
+    __syncthreads();
+  }
+
+  if (odd) {  // the rows that see a value left out get it
+#pragma unroll 1
+    for (uint32_t step = begin; step < end; ++step) {
+      const int32_t t0 = (int32_t)(step * kStep);
+      if (all_see(t0) && !kLeaveOut<T, CODE>) continue;
+#pragma unroll
+      for (int c = 0; c < kChannels; ++c)
+#pragma unroll 1
+        for (int i = 0; i < kTiles; ++i) {
+          const int32_t t = t0 + 32 * i + 16 * (int32_t)half, page = page_of(t);
+          const bool ok = (uint32_t)page < a.c.n_pages;
+          const uint4 w = *(const uint4 *)(a.c.v + ((size_t)(ok ? page : 0) * a.c.heads + pc.head) * page_bytes +
+                                           (size_t)(32 * c + col) * P + ((uint32_t)t & (P - 1)));
+          if (!__any(any_unbounded<CODE>(w))) continue;
+#pragma unroll 1
+          for (int kind = 0; kind < 3; ++kind) {
+            f32x16 hits = {};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              Frag see;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) see.b[j] = (__bf16)(ok && sees(seen, t + 8 * u + j) ? 1.0f : 0.0f);
+              const Frag is = u ? class_frag<CODE>(w.z, w.w, kind) : class_frag<CODE>(w.x, w.y, kind);
+              hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is.b, see.b, hits, 0, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (hits[j] > 0) acc[c][j] += class_value(kind);
+          }
+        }
+    }
+  }
+
+  l += __shfl_xor(l, 32);
+  if (!here) return;
+  const uint32_t in = r - r0;
+  const int64_t row = pc.q.first + (int64_t)tok;
+  Value *out = (Value *)a.out + row * a.out_row + (int64_t)head * a.out_head;
+  const size_t at = (size_t)(pc.slot + pc.split) * F::kRows + in;
+  const float inv = l == 0 ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int c = 0; c < kChannels; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t d = 32 * c + 8 * i + 4 * half;
+      f32x4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = acc[c][4 * i + j];
+      if (pc.splits > 1) *(f32x4 *)(a.part_acc + at * D + d) = x;
+      else store4<T>(out + d, x * inv, a.out_vec);
+    }
+  if (half == 0) {
+    if (pc.splits > 1) {
+      a.part_ml[2 * at] = m;
+      a.part_ml[2 * at + 1] = l;
+    } else if (a.lse) {
+      a.lse[row * a.n_q_heads + head] = l == 0 ? -INFINITY : (m + log2_fast(l)) * 0.6931471805599453f;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ joining pieces
+// Pieces' maxima, sums and accs of the blocks that were split.  A wave takes a row:
+// lanes in groups of dim / 4, four channels to a lane, each group every so many
+// pieces; blockIdx.y tells which rows of the block.
+constexpr uint32_t kJoinRows = 4;
+template <int T, int D>
+__global__ __launch_bounds__(64 * kJoinRows) void join_kernel(AttendArgs a, uint32_t rows, bool last_first, int64_t least, int64_t most) {
+  typedef typename Elem<T>::type Value;
+  constexpr uint32_t kLanes = D / 4, kGroups = 64 / kLanes;
+  static_assert((kGroups & (kGroups - 1)) == 0, "groups add up in halves");
+  Piece pc;
+  if (!find_piece<64 * kJoinRows, true>(a, rows, least, most, blockIdx.x, &pc)) return;
+  const uint32_t lane = threadIdx.x & 63, group = lane / kLanes, d = 4 * (lane % kLanes);
+  const uint32_t list = (uint32_t)pc.q.rows * a.group, in = blockIdx.y * kJoinRows + (threadIdx.x >> 6);
+  const uint32_t r = (last_first ? (list + rows - 1) / rows - 1 - pc.block : pc.block) * rows + in;
+  if (in >= rows || r >= list) return;
+  const float *ml = a.part_ml + 2 * ((size_t)pc.slot * rows + in);
+  float m = -INFINITY;
+  for (uint32_t s = lane; s < pc.splits; s += 64) m = fmaxf(m, ml[2 * (size_t)s * rows]);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  f32x4 acc = {0, 0, 0, 0};
+  float l = 0;
+  if (group < kGroups) {
+#pragma unroll 4
+    for (uint32_t s = group; s < pc.splits; s += kGroups) {
+      const size_t at = (size_t)s * rows;
+      const float ms = ml[2 * at], w = ms == m ? 1.0f : exp2_fast(ms - m);
+      l += w * ml[2 * at + 1];
+      acc += w * *(const f32x4 *)(a.part_acc + ((size_t)pc.slot * rows + in + at) * D + d);
+    }
+  }
+#pragma unroll
+  for (uint32_t o = kGroups / 2; o; o >>= 1) {  // into the first group
+    const int from = (int)(lane + o * kLanes) & 63;
+    l += __shfl(l, from);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += __shfl(acc[j], from);
+  }
+  if (group != 0) return;
+  const int64_t row = pc.q.first + (int64_t)(r / a.group), head = (int64_t)pc.head * a.group + r % a.group;
+  const float inv = l == 0 ? 0.0f : 1.0f / l;
+  store4<T>((Value *)a.out + row * a.out_row + head * a.out_head + d, acc * inv, a.out_vec);
+  if (a.lse && d == 0) a.lse[row * a.n_q_heads + head] = l == 0 ? -INFINITY : (m + log2_fast(l)) * 0.6931471805599453f;
 }
 
 // ------------------------------------------------------------------ launches, by head_dim
@@ -664,6 +1033,10 @@ constexpr uint32_t few_blocks(uint32_t dim, uint64_t list) {
   const uint32_t most = dim <= 128 ? 4 : 2;  // LDS: 16 NM rows of dim fp32 values, twice, in 64 KiB
   return list <= 16 ? 1 : list <= 32 || most == 2 ? 2 : 4;
 }
+// Lists of more rows than this go to the many-rows kernel (fp32 has none: its three
+// terms make the matrix units the bound, which few rows reach as well).
+constexpr uint32_t kManyFrom = 64;
+inline bool many_rows(uzip_dtype type, uint64_t list) { return type != UZIP_FP32 && list > kManyFrom; }
 template <int D>
 uzip_status launch_attend(const AttendCall &call);
 

@@ -1,5 +1,6 @@
 // kv_attend.hip -- attention of new tokens over the 8-bit pages.
 #include <algorithm>
+#include <cmath>
 
 #include "kv_attend.h"
 #include "kv_host.h"
@@ -9,7 +10,13 @@ namespace {
 
 // Pieces of work that fill the GPU: two workgroups for each compute unit.
 uint32_t target_pieces(int cus) { return 2u * (uint32_t)std::max(cus, 1); }
-constexpr uint32_t kMostTarget = 2048;  // what the workspace is sized for, whatever the device
+constexpr uint32_t kMostTarget = 512;  // what the workspace is sized for, whatever the device
+
+// Rows of a slot of the workspace.
+uint64_t slot_rows(uzip_dtype dtype, uint32_t head_dim, uint32_t group, uint32_t max_new) {
+  const uint64_t list = (uint64_t)max_new * group;
+  return many_rows(dtype, list) ? 128 : 16 * few_blocks(head_dim, list);
+}
 
 bool attend_sizes(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_heads, uint32_t n_heads, uint32_t head_dim,
                   uint32_t n_reqs) {
@@ -28,7 +35,7 @@ extern "C" {
 size_t uzip_kv_attend_workspace(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_heads, uint32_t n_heads,
                                 uint32_t head_dim, uint32_t n_reqs, uint32_t max_new) {
   if (!attend_sizes(dtype, n_rows, n_q_heads, n_heads, head_dim, n_reqs)) return 0;
-  const uint64_t rows = 16ull * few_blocks(head_dim, (uint64_t)max_new * (n_q_heads / n_heads));
+  const uint64_t rows = slot_rows(dtype, head_dim, n_q_heads / n_heads, max_new);
   return (size_t)(2 * kMostTarget * rows * (head_dim + 2) * sizeof(float));
 }
 
@@ -72,14 +79,15 @@ uzip_status uzip_kv_attend(const uzip_kv_cache *cache, uzip_dtype dtype, const v
   a.n_reqs = n_reqs;
   a.window = window;
   a.target = std::min(target_pieces(cus), kMostTarget);
-  a.scale_log2 = scale * 1.4426950408889634f;
+  a.scale_log2 = std::fabs(scale) * 1.4426950408889634f;
+  a.negate = scale < 0;
   auto at_multiples = [&](const void *p, int64_t row, int64_t head, int64_t of) {
     return aligned(p, of) && row * bytes % of == 0 && head * bytes % of == 0;
   };
   a.q_vec = at_multiples(d_q, q_row, q_head, 16);
   a.out_vec = at_multiples(d_out, out_row, out_head, 4 * bytes);
   a.part_acc = (float *)d_ws;
-  a.part_ml = a.part_acc + 2ull * kMostTarget * 16 * few_blocks(cache->head_dim, (uint64_t)max_new * a.group) * cache->head_dim;
+  a.part_ml = a.part_acc + 2ull * kMostTarget * slot_rows(dtype, cache->head_dim, a.group, max_new) * cache->head_dim;
   call.type = dtype;
   call.code = cache->dtype;
   call.max_new = max_new;

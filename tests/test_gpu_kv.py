@@ -407,6 +407,57 @@ def test_attend_large_scores(uz):
         attend_case(uz, 16, 64, 1, 2, kind, "e4m3fn", [100], [1], scale=0.0)
 
 
+@pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("new,window", [([6, 1], 0), ([6, 3], 9), ([100, 70], 0), ([90, 1], 33)])
+def test_attend_nan_and_infinity_reach_only_rows_that_see_them(uz, fmt, kind, new, window):
+    say("nan", fmt, kind, new, window)
+    g = np.random.default_rng(71)
+    page, dim, kv, group = 16, 64, 2, 2
+    side = Side(uz, 24, kv, page, dim, fmt, g)
+    total = [130, 75]
+
+    def edit(x, d):
+        for t in (x, d):
+            if x.stride(0) and edit.values:                               # values only: a key's NaN is another test
+                for tok, ch, v in [(124, 3, "nan"), (127, 3, "inf"), (126, 5, "inf"), (128, 6, "-inf"), (129, 6, "inf"), (60, 9, "nan"),
+                                   (40, 11, "inf"), (130 + 72, 1, "nan"), (130 + 20, 2, "-inf")]:
+                    t[tok, 1, ch] = float(v)
+        edit.values = True                                                # grow edits keys first
+    edit.values = False
+    _, want, _ = grow(uz, side, [0, 0], total, np.full((2, 12), -1, np.int32), np.arange(24, dtype=np.int32), kind, g, edit=edit)
+    rows = sum(new)
+    q, qd = rows_of((rows, kv * group, dim), kind, g)
+    q_start = np.array([0, new[0], rows], np.int32)
+    with np.errstate(invalid="ignore"):
+        expect = ref.attend(np_of(q), side.k, side.k_exp, side.v, side.v_exp, fmt, want["table"], total, q_start, page, 0.1, window)
+    out, lse = run_attend(uz, side, qd, ints(want["table"]), ints(total), ints(q_start), max(new), 0.1, window)
+    got, fine = np_of(out), np.isfinite(expect["out"])
+    assert not fine.all() and fine.any()
+    assert np.array_equal(got[~fine], expect["out"][~fine], equal_nan=True)
+    assert np.isfinite(got[fine]).all()
+    clean = {k: np.where(fine, v, 0.0) if k in ("out", "spread") else v for k, v in expect.items()}
+    check_attend((torch.from_numpy(np.where(fine, got, 0.0)), lse), clean, kind, dim, 130)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("new", [[5], [100]])
+def test_attend_nan_keys_reach_only_rows_that_see_them(uz, kind, new):
+    g = np.random.default_rng(72)
+    side = Side(uz, 10, 1, 16, 64, "e4m3fn", g)
+
+    def edit(x, d):
+        for t in (x, d):
+            t[117, 0, 7] = float("nan")
+    _, want, _ = grow(uz, side, [0], [120], np.full((1, 8), -1, np.int32), np.arange(10, dtype=np.int32), kind, g, edit=edit)
+    q, qd = rows_of((new[0], 2, 64), kind, g)
+    out, lse = run_attend(uz, side, qd, ints(want["table"]), ints([120]), ints([0, new[0]]), new[0], 0.1)
+    torch.cuda.synchronize()
+    first = 117 - (120 - new[0])
+    assert torch.isfinite(out[:first]).all() and torch.isfinite(lse[:first]).all()
+    assert torch.isnan(out[first:]).all() and torch.isnan(lse[first:]).all()
+
+
 def test_attend_repeats_its_bits(uz):
     """The same call gives the same bits, on a workspace that holds anything, on another stream, without lse."""
     for new in ([1, 1, 1], [3, 150, 1]):
