@@ -14,6 +14,8 @@
 // unit along the tokens is a step of 64.
 #pragma once
 
+#include <utility>
+
 #include "kv_device.h"
 
 namespace uzip_kv {
@@ -25,8 +27,8 @@ struct AttendArgs {
   float *lse;
   int64_t q_row, q_head, out_row, out_head;
   const int32_t *table, *lens, *q_start;
-  float *part_acc;   // [slot][row of the block][dim]: acc of pieces that are joined
-  float *part_ml;    // [slot][row of the block][2]: their m and l
+  float *part_acc;   // [row][dim]: acc of pieces that are joined, a row for each of their blocks' rows
+  float *part_ml;    // [row][2]: their m and l
   uint32_t n_rows, n_q_heads, group, max_pages, n_reqs, window;
   uint32_t target;   // pieces that fill the GPU
   float scale_log2;  // |scale| log2 e
@@ -39,12 +41,19 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 64;      // tokens of a step
 constexpr int kMinSteps = 4;   // steps of a piece, so each of a workgroup's waves has one
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
+
+// Lists of more rows than this go to the many-rows kernel, in blocks of 128 (fp32
+// has none: its three terms make the matrix units the bound, which few rows reach
+// as well).
+constexpr uint32_t kManyFrom = 64, kManyBlock = 128;
 
 // ------------------------------------------------------------------ pieces of work
 struct Request {
@@ -84,15 +93,23 @@ __device__ __forceinline__ Seen seen_by(const AttendArgs &a, int32_t place) {
 }
 __device__ __forceinline__ bool sees(const Seen &s, int32_t t) { return (uint32_t)t - (uint32_t)s.first <= s.span; }
 
+// The lists that one kernel takes: those of least to most rows, in blocks of rows.
+struct Lists {
+  int64_t least, most;
+  uint32_t rows;
+  uint32_t slots;  // first row of the workspace for their pieces
+};
+
 struct Piece {
   Request q;
   uint32_t req, head, block;     // which rows
-  uint32_t split, splits, slot;  // which part of their tokens; the slot of part 0
+  uint32_t split, splits;        // which part of their tokens
+  size_t part;                   // row of the workspace of part 0's first row; the others follow, a block's rows apart
 };
 
-__device__ __forceinline__ uint32_t blocks_of(const AttendArgs &a, const Request &q, uint32_t rows, int64_t least, int64_t most) {
+__device__ __forceinline__ uint32_t blocks_of(const AttendArgs &a, const Request &q, const Lists &l) {
   const int64_t list = (int64_t)q.rows * a.group;
-  return list >= least && list <= most ? (uint32_t)((list + rows - 1) / rows) : 0u;
+  return list >= l.least && list <= l.most ? (uint32_t)((list + l.rows - 1) / l.rows) : 0u;
 }
 
 // The most steps that a block of `rows` rows of the request can have.
@@ -111,8 +128,7 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
   return x;
 }
 
-// Which piece is number `index`, found by the whole workgroup.  Requests whose
-// list has `least` to `most` rows take part, in blocks of `rows`.  All blocks'
+// Which piece of the lists is number `index`, found by the whole workgroup.  All blocks'
 // steps are shared out so that about `target` pieces of equal length come of
 // them; a block shorter than that stays whole.  With JOIN the index counts the
 // blocks that were split instead.  At most target + blocks pieces, at most
@@ -120,8 +136,9 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
 // steps is split only where n > S, the steps of a piece, into ceil(n / S) <
 // 2 n / S.  Every workgroup sums over the requests for itself: two scans.
 template <int THREADS, bool JOIN>
-__device__ bool find_piece(const AttendArgs &a, uint32_t rows, int64_t least, int64_t most, uint32_t index, Piece *out) {
+__device__ bool find_piece(const AttendArgs &a, const Lists &lists, uint32_t index, Piece *out) {
   constexpr int kWaves = THREADS / 64;
+  const uint32_t rows = lists.rows;
   __shared__ uint64_t part[2 * kWaves];
   __shared__ Piece found;
   const uint32_t tid = threadIdx.x, wave = tid >> 6, n = a.n_reqs + 1;  // with the rows of no request
@@ -129,7 +146,7 @@ __device__ bool find_piece(const AttendArgs &a, uint32_t rows, int64_t least, in
   uint64_t steps = 0;
   for (uint32_t i = lo; i < hi; ++i) {
     const Request q = request(a, i);
-    steps += (uint64_t)blocks_of(a, q, rows, least, most) * steps_of(a, q, rows);
+    steps += (uint64_t)blocks_of(a, q, lists) * steps_of(a, q, rows);
   }
   steps = wave_scan64(steps);
   if ((tid & 63) == 63) part[wave] = steps;
@@ -140,7 +157,7 @@ __device__ bool find_piece(const AttendArgs &a, uint32_t rows, int64_t least, in
   all *= a.c.heads;
   const uint64_t length = max((all + a.target - 1) / a.target, (uint64_t)kMinSteps);  // S
   auto count = [&](const Request &q, uint32_t *splits) {
-    const uint32_t b = blocks_of(a, q, rows, least, most);
+    const uint32_t b = blocks_of(a, q, lists);
     *splits = (uint32_t)max((steps_of(a, q, rows) + length - 1) / length, (uint64_t)1);
     const uint64_t pieces = (uint64_t)b * a.c.heads * (JOIN ? (*splits > 1 ? 1u : 0u) : *splits);
     return pieces | (*splits > 1 ? (uint64_t)b * a.c.heads * *splits : 0) << 32;  // pieces; slots
@@ -171,7 +188,7 @@ __device__ bool find_piece(const AttendArgs &a, uint32_t rows, int64_t least, in
       p.split = JOIN ? 0 : up % splits;
       p.splits = splits;
       p.block = JOIN ? up : up / splits;
-      p.slot = (uint32_t)(at >> 32) + (p.block * a.c.heads + p.head) * splits;
+      p.part = lists.slots + ((at >> 32) + (uint64_t)(p.block * a.c.heads + p.head) * splits) * rows;
       found = p;
     }
     at += c;
@@ -179,6 +196,16 @@ __device__ bool find_piece(const AttendArgs &a, uint32_t rows, int64_t least, in
   __syncthreads();
   *out = found;
   return true;
+}
+
+// f(0), f(1), ... f(N - 1), the arguments constants: arrays that f indexes with them stay in registers.
+template <int... I, class F>
+__device__ __forceinline__ void static_for(std::integer_sequence<int, I...>, const F &f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(const F &f) {
+  static_for(std::make_integer_sequence<int, N>{}, f);
 }
 
 // ------------------------------------------------------------------ fragments
@@ -210,7 +237,7 @@ union Frag {
   f16x8 h;
   bf16x2 b2[4];
   f16x2 h2[4];
-  uint4 u;
+  u32x4 u;
 };
 
 // Eight codes (two words) as a fragment, times 2^(e - 127) where scale = 2^(e - 127).
@@ -283,7 +310,7 @@ __device__ __forceinline__ void query_frag(const typename Elem<T>::type *x, bool
         v[j] -= (float)f[i].b[j];
       }
   } else if (wide) {
-    f[0].u = *(const uint4 *)x;
+    f[0].u = *(const u32x4 *)x;
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -293,7 +320,7 @@ __device__ __forceinline__ void query_frag(const typename Elem<T>::type *x, bool
   }
   if (negate) {
 #pragma unroll
-    for (int i = 0; i < Query<T>::kTerms; ++i) f[i].u = uint4{f[i].u.x ^ 0x80008000u, f[i].u.y ^ 0x80008000u, f[i].u.z ^ 0x80008000u, f[i].u.w ^ 0x80008000u};
+    for (int i = 0; i < Query<T>::kTerms; ++i) f[i].u = u32x4{f[i].u.x ^ 0x80008000u, f[i].u.y ^ 0x80008000u, f[i].u.z ^ 0x80008000u, f[i].u.w ^ 0x80008000u};
   }
 }
 
@@ -319,8 +346,8 @@ __device__ __forceinline__ void store4(typename Elem<T>::type *out, f32x4 x, boo
 #pragma unroll
   for (int j = 0; j < 4; ++j) o[j] = (Value)x[j];
   if (wide) {
-    if constexpr (sizeof(Value) == 2) *(uint2 *)out = *(uint2 *)o;
-    else *(uint4 *)out = *(uint4 *)o;
+    if constexpr (sizeof(Value) == 2) *(u32x2 *)out = *(u32x2 *)o;
+    else *(u32x4 *)out = *(u32x4 *)o;
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) out[j] = o[j];
@@ -333,12 +360,12 @@ __device__ __forceinline__ uint32_t bounded(uint32_t w) {
   return w & ~((unbounded<CODE>(w) >> 7) * 0xFFu);
 }
 template <int CODE>
-__device__ __forceinline__ bool any_unbounded(uint4 w) {
+__device__ __forceinline__ bool any_unbounded(u32x4 w) {
   return (unbounded<CODE>(w.x) | unbounded<CODE>(w.y) | unbounded<CODE>(w.z) | unbounded<CODE>(w.w)) != 0;
 }
 template <int CODE>
-__device__ __forceinline__ uint4 bounded(uint4 w) {
-  return uint4{bounded<CODE>(w.x), bounded<CODE>(w.y), bounded<CODE>(w.z), bounded<CODE>(w.w)};
+__device__ __forceinline__ u32x4 bounded(u32x4 w) {
+  return u32x4{bounded<CODE>(w.x), bounded<CODE>(w.y), bounded<CODE>(w.z), bounded<CODE>(w.w)};
 }
 
 // 1 for each of the eight codes that is NaN (kind 0), infinite (1) or minus
@@ -371,14 +398,14 @@ struct FewRows {
 };
 
 template <int T, int CODE, int D, int NM>
-__global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t least, int64_t most) {
+__device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index) {
   typedef FewRows<D, NM> F;
   typedef typename Elem<T>::type Value;
   constexpr int TERMS = Query<T>::kTerms, PROBS = Query<T>::kProbs;
   __shared__ float join_acc[2][F::kRows][D + 4];
   __shared__ float join_ml[F::kWaves][F::kRows][2];
   Piece pc;
-  if (!find_piece<F::kThreads, false>(a, F::kRows, least, most, blockIdx.x, &pc)) return;
+  if (!find_piece<F::kThreads, false>(a, lists, index, &pc)) return;
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
   const uint32_t list = (uint32_t)pc.q.rows * a.group, r0 = pc.block * F::kRows, P = a.c.page;
   int32_t lo, hi;
@@ -425,8 +452,8 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
   // page of the 16 tokens from t on; -1 past the tokens
   auto page_of = [&](int32_t t) { return t < hi ? table[(uint32_t)t >> a.c.page_shift] : -1; };
   const int32_t key_chunk = 16 * (int32_t)(col >> 2), value_chunk = 16 * (int32_t)g;
-  uint4 k16[4][F::kPairs > 0 ? F::kPairs : 1], v16[F::kChannels];
-  uint2 k8[4];
+  u32x4 k16[4][F::kPairs > 0 ? F::kPairs : 1], v16[F::kChannels];
+  u32x2 k8[4];
   uint32_t e_k, e_v;
   bool page_here;
   auto load_keys = [&](int32_t t0, int32_t page) {
@@ -436,8 +463,8 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
-      for (int s = 0; s < F::kPairs; ++s) k16[i][s] = *(const uint4 *)(row + i * 4 * D + 64 * s + 16 * g);
-      if (F::kOdd) k8[i] = *(const uint2 *)(row + i * 4 * D + 64 * F::kPairs + 8 * g);
+      for (int s = 0; s < F::kPairs; ++s) k16[i][s] = *(const u32x4 *)(row + i * 4 * D + 64 * s + 16 * g);
+      if (F::kOdd) k8[i] = *(const u32x2 *)(row + i * 4 * D + 64 * F::kPairs + 8 * g);
     }
   };
   auto load_values = [&](int32_t t0, int32_t page) {
@@ -445,7 +472,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
     const size_t ph = (size_t)(page_here ? page : 0) * a.c.heads + pc.head;
     const uint8_t *at = a.c.v + ph * page_bytes + (size_t)col * P + ((uint32_t)(t0 + value_chunk) & (P - 1));
 #pragma unroll
-    for (int c = 0; c < F::kChannels; ++c) v16[c] = *(const uint4 *)(at + (size_t)16 * c * P);
+    for (int c = 0; c < F::kChannels; ++c) v16[c] = *(const u32x4 *)(at + (size_t)16 * c * P);
     e_k = a.c.k_exp[ph];
     e_v = a.c.v_exp[ph];
   };
@@ -476,7 +503,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
       for (int ks = 0; ks < F::kKeySteps; ++ks) {
         Frag k;
         if (ks < 2 * F::kPairs) {
-          const uint4 w = k16[i][ks / 2];
+          const u32x4 w = k16[i][ks / 2];
           k = ks % 2 ? key_frag<T, CODE>(w.z, w.w) : key_frag<T, CODE>(w.x, w.y);
         } else {
           k = key_frag<T, CODE>(k8[i].x, k8[i].y);
@@ -546,7 +573,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
     if (!whole || kLeaveOut<T, CODE>) {
 #pragma unroll
       for (int c = 0; c < F::kChannels; ++c) {
-        uint4 w = v16[c];
+        u32x4 w = v16[c];
         if (!whole) {
           w.x = page_ok ? keep_tokens(w.x, t_lane, lo, hi) : 0u;
           w.y = page_ok ? keep_tokens(w.y, t_lane + 4, lo, hi) : 0u;
@@ -563,7 +590,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
 
 #pragma unroll
     for (int c = 0; c < F::kChannels; ++c) {
-      const uint4 w = v16[c];
+      const u32x4 w = v16[c];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const Frag v = u ? codes_bf16<CODE>(w.z, w.w, vs) : codes_bf16<CODE>(w.x, w.y, vs);
@@ -661,7 +688,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a, int64_t l
     const uint32_t in = 16 * n + col, r = r0 + in;
     if (r >= list) continue;
     if (pc.splits > 1) {
-      const size_t at = (size_t)(pc.slot + pc.split) * F::kRows + in;
+      const size_t at = pc.part + (size_t)pc.split * F::kRows + in;
 #pragma unroll
       for (int c = 0; c < F::kChannels; ++c) *(f32x4 *)(a.part_acc + at * D + 16 * c + 4 * g) = acc[n][c];
       if (g == 0) {
@@ -696,6 +723,7 @@ struct ManyRows {
   static constexpr int kChunks = D / 16;              // of a key, and blocks of 16 channels
   static constexpr int kAll = kStep * kChunks, kLoads = (kAll + kThreads - 1) / kThreads;  // chunks of keys; of each thread; as many of values
   __device__ static __forceinline__ bool has(uint32_t n) { return kAll % kThreads == 0 || n < kAll; }
+  static constexpr int kRing = 2, kPages = 4;         // steps in LDS: codes; their pages
   // Chunk c of token t of a step, and chunk c (16 tokens) of channel d, in units of 16 bytes.
   __device__ static __forceinline__ uint32_t key_at(uint32_t t, uint32_t c) {
     uint32_t turn;
@@ -716,16 +744,17 @@ __device__ __forceinline__ f32x16 score_mfma32(const Frag &k, const Frag &q, f32
 }
 
 template <int T, int CODE, int D>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_many_kernel(AttendArgs a, int64_t least, int64_t most) {
+__device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t index) {
   typedef ManyRows<D> F;
   typedef typename Elem<T>::type Value;
   constexpr int PROBS = Query<T>::kProbs, kTiles = kStep / 32, kChannels = D / 32, kKeySteps = D / 16;
-  __shared__ uint4 keys[2][F::kAll];
-  __shared__ uint4 values[2][F::kAll];
-  __shared__ float key_scale[2][4], value_scale[2][4];  // of 16 tokens each; a key's is -1 where there is no page
+  __shared__ u32x4 keys[F::kRing][F::kAll];
+  __shared__ u32x4 values[F::kRing][F::kAll];
+  __shared__ float key_scale[F::kRing][4], value_scale[F::kRing][4];  // of 16 tokens each; a key's is -1 where there is no page
+  __shared__ int32_t step_page[F::kPages][4];        // pages of 16 tokens each
   __shared__ uint32_t odd;                              // a NaN or an infinity was left out
   Piece pc;
-  if (!find_piece<F::kThreads, false>(a, F::kRows, least, most, blockIdx.x, &pc)) return;
+  if (!find_piece<F::kThreads, false>(a, lists, index, &pc)) return;
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
   const uint32_t list = (uint32_t)pc.q.rows * a.group, P = a.c.page;
   // the blocks with the most tokens first: the last ones to run are short
@@ -758,69 +787,91 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_many_kernel(Atte
   // staging: thread's chunks n = tid + 256 i
   const int32_t *table = a.table + (size_t)pc.req * a.max_pages;
   const size_t page_bytes = (size_t)P * D;
-  uint4 stage_k[F::kLoads], stage_v[F::kLoads];
-  float stage_scale = 0;
+  u32x4 stage_k[F::kLoads], stage_v[F::kLoads];
+  uint32_t stage_exp = 0;
+  bool exp_ok = true;
   const int32_t b_min = pc.q.base + (int32_t)(r0 / a.group), b_max = pc.q.base + (int32_t)((min(list, r0 + F::kRows) - 1) / a.group);
   auto all_see = [&](int32_t t0) {  // all rows of the block
     return t0 + kStep - 1 <= b_min && (a.window == 0 || (int64_t)t0 > (int64_t)b_max - a.window);
   };
   auto page_of = [&](int32_t t) { return t < hi ? table[(uint32_t)t >> a.c.page_shift] : -1; };
+  // A step's pages are looked up a step before its codes are asked for, and those
+  // are looked at only when they are put into LDS, after the products of another
+  // step: nothing waits for memory that has not had a step's time.
+  bool stage_ok = true;
+  int32_t next_page = -1;
   auto load = [&](uint32_t step) {
     const int32_t t0 = (int32_t)(step * kStep);
-    const bool edge = !all_see(t0);
+    const int32_t *pages = step_page[step % F::kPages];
+    const uint8_t *k_at[F::kLoads], *v_at[F::kLoads];
+    if (P >= kStep) {  // one page: its address is the same in all lanes
+      const int32_t page = __builtin_amdgcn_readfirstlane(pages[0]);
+      stage_ok = (uint32_t)page < a.c.n_pages;
+      const size_t at = ((size_t)(stage_ok ? page : 0) * a.c.heads + pc.head) * page_bytes;
+      const uint32_t in = (uint32_t)t0 & (P - 1);
 #pragma unroll
-    for (int i = 0; i < F::kLoads; ++i) {
-      const uint32_t n = tid + F::kThreads * i, t = n / F::kChunks, c = n % F::kChunks;
-      if (!F::has(n)) break;
-      int32_t page = page_of(t0 + (int32_t)(t & ~15u));
-      page = (uint32_t)page < a.c.n_pages ? page : 0;
-      stage_k[i] = *(const uint4 *)(a.c.k + ((size_t)page * a.c.heads + pc.head) * page_bytes +
-                                    (((uint32_t)t0 + t) & (P - 1)) * D + 16 * c);
+      for (int i = 0; i < F::kLoads; ++i) {
+        const uint32_t n = tid + F::kThreads * i;
+        k_at[i] = a.c.k + at + (size_t)in * D + 16 * n;
+        v_at[i] = a.c.v + at + in + ((n / 4) * P + 16 * (n % 4));
+      }
+    } else {
+      const int32_t value_page = pages[tid % 4];
+      stage_ok = (uint32_t)value_page < a.c.n_pages;
+      const uint8_t *v = a.c.v + ((size_t)(stage_ok ? value_page : 0) * a.c.heads + pc.head) * page_bytes + (16 * (tid % 4) & (P - 1));
+#pragma unroll
+      for (int i = 0; i < F::kLoads; ++i) {
+        const uint32_t n = tid + F::kThreads * i, t = n / F::kChunks, c = n % F::kChunks;
+        int32_t page = pages[F::has(n) ? t / 16 : 0];
+        page = (uint32_t)page < a.c.n_pages ? page : 0;
+        k_at[i] = a.c.k + ((size_t)page * a.c.heads + pc.head) * page_bytes + (t & (P - 1)) * D + 16 * c;
+        v_at[i] = v + (n / 4) * P;
+      }
     }
 #pragma unroll
-    for (int i = 0; i < F::kLoads; ++i) {
-      const uint32_t n = tid + F::kThreads * i, d = n / 4, c = n % 4;
-      if (!F::has(n)) break;
-      const int32_t t = t0 + 16 * (int32_t)c, page = page_of(t);
-      const bool ok = (uint32_t)page < a.c.n_pages;
-      uint4 w = *(const uint4 *)(a.c.v + ((size_t)(ok ? page : 0) * a.c.heads + pc.head) * page_bytes + (size_t)d * P +
-                                 ((uint32_t)t & (P - 1)));
-      if (!ok) w = uint4{0, 0, 0, 0};
-      if (edge) {  // codes that no row sees count as zero, for 0 times NaN is not 0
-        w.x = keep_tokens(w.x, t, lo, hi);
-        w.y = keep_tokens(w.y, t + 4, lo, hi);
-        w.z = keep_tokens(w.z, t + 8, lo, hi);
-        w.w = keep_tokens(w.w, t + 12, lo, hi);
+    for (int i = 0; i < F::kLoads; ++i)
+      if (F::has(tid + F::kThreads * i)) {
+        stage_k[i] = *(const u32x4 *)k_at[i];
+        stage_v[i] = *(const u32x4 *)v_at[i];
       }
-      if (edge || kLeaveOut<T, CODE>) {
-        if (any_unbounded<CODE>(w)) {  // seen by some rows perhaps: left for after the loop
-          odd = 1;
-          w = bounded<CODE>(w);
-        }
-      }
-      stage_v[i] = w;
-    }
     if (tid < 8) {
-      const int32_t page = page_of(t0 + 16 * (int32_t)(tid & 3));
+      const int32_t page = pages[tid & 3];
       const bool ok = (uint32_t)page < a.c.n_pages;
       const size_t ph = (size_t)(ok ? page : 0) * a.c.heads + pc.head;
-      const float s = pow2((tid < 4 ? a.c.k_exp : a.c.v_exp)[ph]);
-      stage_scale = ok ? s : tid < 4 ? -1.0f : 1.0f;
+      stage_exp = (tid < 4 ? a.c.k_exp : a.c.v_exp)[ph];
+      exp_ok = ok;
     }
+    if (tid < 4) next_page = page_of(t0 + kStep + 16 * (int32_t)tid);
+  };
+  auto put_one = [&](uint32_t b, int32_t t, bool edge, uint32_t n, const u32x4 &k, u32x4 w) {
+    if (!F::has(n)) return;
+    keys[b][F::key_at(n / F::kChunks, n % F::kChunks)] = k;
+    if (edge) {  // codes that no row sees count as zero, for 0 times NaN is not 0
+      w.x = stage_ok ? keep_tokens(w.x, t, lo, hi) : 0u;
+      w.y = stage_ok ? keep_tokens(w.y, t + 4, lo, hi) : 0u;
+      w.z = stage_ok ? keep_tokens(w.z, t + 8, lo, hi) : 0u;
+      w.w = stage_ok ? keep_tokens(w.w, t + 12, lo, hi) : 0u;
+    }
+    if (edge || kLeaveOut<T, CODE>) {
+      if (any_unbounded<CODE>(w)) odd = 1;  // seen by some rows perhaps: left for after the loop
+      w = bounded<CODE>(w);
+    }
+    values[b][F::value_at(n / 4, n % 4)] = w;
   };
   auto put = [&](uint32_t step) {
-    const uint32_t b = step & 1;
-#pragma unroll
-    for (int i = 0; i < F::kLoads; ++i) {
-      const uint32_t n = tid + F::kThreads * i;
-      if (!F::has(n)) break;
-      keys[b][F::key_at(n / F::kChunks, n % F::kChunks)] = stage_k[i];
-      values[b][F::value_at(n / 4, n % 4)] = stage_v[i];
+    const uint32_t b = step % F::kRing;
+    const int32_t t0 = (int32_t)(step * kStep), t = t0 + 16 * (int32_t)(tid % 4);
+    const bool edge = !all_see(t0) || !__all(stage_ok);
+    static_for<F::kLoads>([&](auto i) { put_one(b, t, edge, tid + F::kThreads * i, stage_k[i], stage_v[i]); });
+    if (tid < 4) {
+      key_scale[b][tid] = exp_ok ? pow2((int)stage_exp) : -1.0f;
+      step_page[(step + 1) % F::kPages][tid] = next_page;
+    } else if (tid < 8) {
+      value_scale[b][tid - 4] = exp_ok ? pow2((int)stage_exp) : 1.0f;
     }
-    if (tid < 4) key_scale[b][tid] = stage_scale;
-    else if (tid < 8) value_scale[b][tid - 4] = stage_scale;
   };
   if (tid == 0) odd = 0;
+  if (tid < 4) step_page[begin % F::kPages][tid] = page_of((int32_t)(begin * kStep) + 16 * (int32_t)tid);
   __syncthreads();
   if (begin < end) {
     load(begin);
@@ -829,21 +880,25 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_many_kernel(Atte
   __syncthreads();
   const uint32_t key_row = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);  // token of this lane's row
   for (uint32_t step = begin; step < end; ++step) {
-    const uint32_t b = step & 1;
+    const uint32_t b = step % F::kRing;
     const int32_t t0 = (int32_t)(step * kStep);
     if (step + 1 < end) load(step + 1);
     if (w0 < list && t0 <= p_max && (a.window == 0 || (int64_t)t0 + kStep - 1 > (int64_t)p_min - a.window)) {
       f32x16 s[kTiles];
+      // The scores' products are issued before the other waves' softmax, which fills
+      // the gaps between them (with: 703 us, without: 717, a prompt of 8192).
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
         s[i] = f32x16{};
 #pragma unroll
         for (int c = 0; c < kChannels; ++c) {
-          const uint4 w = keys[b][F::key_at(32 * i + key_row, 2 * c + half)];
+          const u32x4 w = keys[b][F::key_at(32 * i + key_row, 2 * c + half)];
           s[i] = score_mfma32<T>(key_frag<T, CODE>(w.x, w.y), q[2 * c], s[i]);
           s[i] = score_mfma32<T>(key_frag<T, CODE>(w.z, w.w), q[2 * c + 1], s[i]);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
       float ks[kTiles], vs[kTiles];  // ks: what a score is still to be multiplied by
       bool page_ok[kTiles], pages_ok = true;
 #pragma unroll
@@ -896,10 +951,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_many_kernel(Atte
           }
         }
 #pragma unroll
-      for (int c = 0; c < kChannels; ++c)
+      for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          const uint4 w = values[b][F::value_at(32 * c + col, 2 * i + half)];
+        for (int c = 0; c < kChannels; ++c) {
+          const u32x4 w = values[b][F::value_at(32 * c + col, 2 * i + half)];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const Frag v = u ? codes_bf16<CODE>(w.z, w.w, vs[i]) : codes_bf16<CODE>(w.x, w.y, vs[i]);
@@ -909,7 +964,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_many_kernel(Atte
           }
         }
     }
-    // the other buffer was last read in the step before, which every wave has left
+    // the other slot was last read in the step before, which every wave has left
     if (step + 1 < end) put(step + 1);
     __syncthreads();
   }
@@ -925,7 +980,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_many_kernel(Atte
         for (int i = 0; i < kTiles; ++i) {
           const int32_t t = t0 + 32 * i + 16 * (int32_t)half, page = page_of(t);
           const bool ok = (uint32_t)page < a.c.n_pages;
-          const uint4 w = *(const uint4 *)(a.c.v + ((size_t)(ok ? page : 0) * a.c.heads + pc.head) * page_bytes +
+          const u32x4 w = *(const u32x4 *)(a.c.v + ((size_t)(ok ? page : 0) * a.c.heads + pc.head) * page_bytes +
                                            (size_t)(32 * c + col) * P + ((uint32_t)t & (P - 1)));
           if (!__any(any_unbounded<CODE>(w))) continue;
 #pragma unroll 1
@@ -952,7 +1007,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_many_kernel(Atte
   const uint32_t in = r - r0;
   const int64_t row = pc.q.first + (int64_t)tok;
   Value *out = (Value *)a.out + row * a.out_row + (int64_t)head * a.out_head;
-  const size_t at = (size_t)(pc.slot + pc.split) * F::kRows + in;
+  const size_t at = pc.part + (size_t)pc.split * F::kRows + in;
   const float inv = l == 0 ? 0.0f : 1.0f / l;
 #pragma unroll
   for (int c = 0; c < kChannels; ++c)
@@ -976,49 +1031,72 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_many_kernel(Atte
 }
 
 // ------------------------------------------------------------------ joining pieces
-// Pieces' maxima, sums and accs of the blocks that were split.  A wave takes a row:
-// lanes in groups of dim / 4, four channels to a lane, each group every so many
-// pieces; blockIdx.y tells which rows of the block.
-constexpr uint32_t kJoinRows = 4;
+// Pieces' maxima, sums and accs of the blocks that were split.  A wave takes a row
+// at a time: lanes in groups of dim / 4, four channels to a lane, each group every
+// so many pieces; `part` tells which 16 rows of the block.
+constexpr uint32_t kJoinRows = 16;
 template <int T, int D>
-__global__ __launch_bounds__(64 * kJoinRows) void join_kernel(AttendArgs a, uint32_t rows, bool last_first, int64_t least, int64_t most) {
+__device__ void join_rows(const AttendArgs &a, const Lists &lists, bool last_first, uint32_t index, uint32_t part) {
   typedef typename Elem<T>::type Value;
-  constexpr uint32_t kLanes = D / 4, kGroups = 64 / kLanes;
+  constexpr uint32_t kLanes = D / 4, kGroups = 64 / kLanes, kWaves = 4;
   static_assert((kGroups & (kGroups - 1)) == 0, "groups add up in halves");
   Piece pc;
-  if (!find_piece<64 * kJoinRows, true>(a, rows, least, most, blockIdx.x, &pc)) return;
-  const uint32_t lane = threadIdx.x & 63, group = lane / kLanes, d = 4 * (lane % kLanes);
-  const uint32_t list = (uint32_t)pc.q.rows * a.group, in = blockIdx.y * kJoinRows + (threadIdx.x >> 6);
-  const uint32_t r = (last_first ? (list + rows - 1) / rows - 1 - pc.block : pc.block) * rows + in;
-  if (in >= rows || r >= list) return;
-  const float *ml = a.part_ml + 2 * ((size_t)pc.slot * rows + in);
-  float m = -INFINITY;
-  for (uint32_t s = lane; s < pc.splits; s += 64) m = fmaxf(m, ml[2 * (size_t)s * rows]);
+  if (!find_piece<64 * kWaves, true>(a, lists, index, &pc)) return;
+  const uint32_t lane = threadIdx.x & 63, group = lane / kLanes, d = 4 * (lane % kLanes), rows = lists.rows;
+  const uint32_t list = (uint32_t)pc.q.rows * a.group;
+  const uint32_t r0 = (last_first ? (list + rows - 1) / rows - 1 - pc.block : pc.block) * rows;
+  const uint32_t end = min(min(rows, list - r0), (part + 1) * kJoinRows);
+  for (uint32_t in = part * kJoinRows + (threadIdx.x >> 6); in < end; in += kWaves) {
+    const uint32_t r = r0 + in;
+    const float *ml = a.part_ml + 2 * (pc.part + in);
+    const float *accs = a.part_acc + (pc.part + in) * D + d;
+    float m = -INFINITY;
+    for (uint32_t s = lane; s < pc.splits; s += 64) m = fmaxf(m, ml[2 * (size_t)s * rows]);
 #pragma unroll
-  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  f32x4 acc = {0, 0, 0, 0};
-  float l = 0;
-  if (group < kGroups) {
+    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    f32x4 acc = {0, 0, 0, 0};
+    float l = 0;
+    if (group < kGroups) {
 #pragma unroll 4
-    for (uint32_t s = group; s < pc.splits; s += kGroups) {
-      const size_t at = (size_t)s * rows;
-      const float ms = ml[2 * at], w = ms == m ? 1.0f : exp2_fast(ms - m);
-      l += w * ml[2 * at + 1];
-      acc += w * *(const f32x4 *)(a.part_acc + ((size_t)pc.slot * rows + in + at) * D + d);
+      for (uint32_t s = group; s < pc.splits; s += kGroups) {
+        const size_t at = (size_t)s * rows;
+        const float ms = ml[2 * at], w = ms == m ? 1.0f : exp2_fast(ms - m);
+        l += w * ml[2 * at + 1];
+        acc += w * *(const f32x4 *)(accs + at * D);
+      }
     }
-  }
 #pragma unroll
-  for (uint32_t o = kGroups / 2; o; o >>= 1) {  // into the first group
-    const int from = (int)(lane + o * kLanes) & 63;
-    l += __shfl(l, from);
+    for (uint32_t o = kGroups / 2; o; o >>= 1) {  // into the first group
+      const int from = (int)(lane + o * kLanes) & 63;
+      l += __shfl(l, from);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] += __shfl(acc[j], from);
+      for (int j = 0; j < 4; ++j) acc[j] += __shfl(acc[j], from);
+    }
+    if (group != 0) continue;
+    const int64_t row = pc.q.first + (int64_t)(r / a.group), head = (int64_t)pc.head * a.group + r % a.group;
+    const float inv = l == 0 ? 0.0f : 1.0f / l;
+    store4<T>((Value *)a.out + row * a.out_row + head * a.out_head + d, acc * inv, a.out_vec);
+    if (a.lse && d == 0) a.lse[row * a.n_q_heads + head] = l == 0 ? -INFINITY : (m + log2_fast(l)) * 0.6931471805599453f;
   }
-  if (group != 0) return;
-  const int64_t row = pc.q.first + (int64_t)(r / a.group), head = (int64_t)pc.head * a.group + r % a.group;
-  const float inv = l == 0 ? 0.0f : 1.0f / l;
-  store4<T>((Value *)a.out + row * a.out_row + head * a.out_head + d, acc * inv, a.out_vec);
-  if (a.lse && d == 0) a.lse[row * a.n_q_heads + head] = l == 0 ? -INFINITY : (m + log2_fast(l)) * 0.6931471805599453f;
+}
+
+// ------------------------------------------------------------------ kernels
+template <int T, int CODE, int D, int NM>
+__global__ __launch_bounds__(256) void few_rows_kernel(AttendArgs a, Lists few) {
+  few_rows<T, CODE, D, NM>(a, few, blockIdx.x);
+}
+// Long lists and short ones in one launch: the first workgroups take the pieces of
+// the long ones, and the short ones' fill the gaps as they end.
+template <int T, int CODE, int D, int NM>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void all_rows_kernel(AttendArgs a, Lists many, uint32_t n_many, Lists few) {
+  if (blockIdx.x < n_many) many_rows<T, CODE, D>(a, many, blockIdx.x);
+  else few_rows<T, CODE, D, NM>(a, few, blockIdx.x - n_many);
+}
+template <int T, int D>
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, Lists many, uint32_t n_many, Lists few) {
+  const uint32_t of_many = kManyBlock / kJoinRows, of_few = few.rows / kJoinRows, i = blockIdx.x - n_many * of_many;
+  if (blockIdx.x < n_many * of_many) join_rows<T, D>(a, many, true, blockIdx.x / of_many, blockIdx.x % of_many);
+  else join_rows<T, D>(a, few, false, i / of_few, i % of_few);
 }
 
 // ------------------------------------------------------------------ launches, by head_dim
@@ -1028,15 +1106,24 @@ struct AttendCall {
   uint32_t max_new;
   hipStream_t stream;
 };
-// Rows of a block of the few-rows kernel for lists of `list` rows.
+// Blocks of 16 rows that a workgroup of the few-rows kernel takes at once, for lists
+// of `list` rows.
 constexpr uint32_t few_blocks(uint32_t dim, uint64_t list) {
   const uint32_t most = dim <= 128 ? 4 : 2;  // LDS: 16 NM rows of dim fp32 values, twice, in 64 KiB
   return list <= 16 ? 1 : list <= 32 || most == 2 ? 2 : 4;
 }
-// Lists of more rows than this go to the many-rows kernel (fp32 has none: its three
-// terms make the matrix units the bound, which few rows reach as well).
-constexpr uint32_t kManyFrom = 64;
-inline bool many_rows(uzip_dtype type, uint64_t list) { return type != UZIP_FP32 && list > kManyFrom; }
+// What a call launches and where its pieces go.
+struct Layout {
+  bool many;              // the kernel for both, with blocks of 16 rows for the short lists
+  uint32_t few;           // blocks of 16 rows to a workgroup
+  uint64_t rows_for_one;  // workspace rows for each slot of the target's 2 * target
+};
+inline Layout layout(uzip_dtype type, uint32_t dim, uint32_t group, uint32_t max_new) {
+  const uint64_t list = (uint64_t)max_new * group;
+  const bool many = type != UZIP_FP32 && list > kManyFrom;
+  const uint32_t few = many ? 1 : few_blocks(dim, list);
+  return {many, few, (many ? kManyBlock : 0) + 16ull * few};
+}
 template <int D>
 uzip_status launch_attend(const AttendCall &call);
 

@@ -12,12 +12,6 @@ namespace {
 uint32_t target_pieces(int cus) { return 2u * (uint32_t)std::max(cus, 1); }
 constexpr uint32_t kMostTarget = 512;  // what the workspace is sized for, whatever the device
 
-// Rows of a slot of the workspace.
-uint64_t slot_rows(uzip_dtype dtype, uint32_t head_dim, uint32_t group, uint32_t max_new) {
-  const uint64_t list = (uint64_t)max_new * group;
-  return many_rows(dtype, list) ? 128 : 16 * few_blocks(head_dim, list);
-}
-
 bool attend_sizes(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_heads, uint32_t n_heads, uint32_t head_dim,
                   uint32_t n_reqs) {
   return valid_type(dtype) && valid_dim(head_dim) && n_heads > 0 && n_q_heads > 0 && n_q_heads % n_heads == 0 &&
@@ -35,8 +29,8 @@ extern "C" {
 size_t uzip_kv_attend_workspace(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_heads, uint32_t n_heads,
                                 uint32_t head_dim, uint32_t n_reqs, uint32_t max_new) {
   if (!attend_sizes(dtype, n_rows, n_q_heads, n_heads, head_dim, n_reqs)) return 0;
-  const uint64_t rows = slot_rows(dtype, head_dim, n_q_heads / n_heads, max_new);
-  return (size_t)(2 * kMostTarget * rows * (head_dim + 2) * sizeof(float));
+  const Layout at = layout(dtype, head_dim, n_q_heads / n_heads, max_new);
+  return (size_t)(2 * kMostTarget * at.rows_for_one * (head_dim + 2) * sizeof(float));
 }
 
 uzip_status uzip_kv_attend(const uzip_kv_cache *cache, uzip_dtype dtype, const void *d_q, int64_t q_row,
@@ -87,7 +81,7 @@ uzip_status uzip_kv_attend(const uzip_kv_cache *cache, uzip_dtype dtype, const v
   a.q_vec = at_multiples(d_q, q_row, q_head, 16);
   a.out_vec = at_multiples(d_out, out_row, out_head, 4 * bytes);
   a.part_acc = (float *)d_ws;
-  a.part_ml = a.part_acc + 2ull * kMostTarget * slot_rows(dtype, cache->head_dim, a.group, max_new) * cache->head_dim;
+  a.part_ml = a.part_acc + 2ull * kMostTarget * layout(dtype, cache->head_dim, a.group, max_new).rows_for_one * cache->head_dim;
   call.type = dtype;
   call.code = cache->dtype;
   call.max_new = max_new;

@@ -7,44 +7,47 @@
 
 namespace uzip_kv {
 
-// Work for one kernel: lists of `least` to `most` rows in blocks of `rows`.
-struct Share {
-  uint32_t rows, grid, joins;  // workgroups: pieces, and blocks that can be split
-  int64_t least, most;
-};
-
-static Share share_of(const AttendArgs &a, uint32_t rows, int64_t least, int64_t most) {
-  // blocks: full ones and a last one for each list, or what lists of `most` can have
+// At most how many pieces, and how many split blocks, find_piece makes of the lists.
+static uint32_t blocks_bound(const AttendArgs &a, const Lists &l) {
+  // full blocks and a last one for each list, or what lists of l.most rows can have
   const uint64_t lists = a.n_reqs + 1, all = (uint64_t)a.n_rows * a.group;
-  const uint64_t each = most < (int64_t)all ? ((uint64_t)most + rows - 1) / rows : UINT64_MAX / lists;
-  const uint64_t blocks = a.c.heads * std::min(all / rows + lists, lists * each);
-  return {rows, (uint32_t)(blocks + a.target), (uint32_t)std::min<uint64_t>(blocks, a.target), least, most};
+  const uint64_t each = l.most < (int64_t)all ? ((uint64_t)l.most + l.rows - 1) / l.rows : UINT32_MAX;
+  return (uint32_t)(a.c.heads * std::min(all / l.rows + lists, lists * each));
 }
 
-template <int T, int CODE>
-static void launch_few(const AttendCall &c, uint32_t blocks, int64_t most) {
-  const AttendArgs &a = c.a;
-  const Share s = share_of(a, 16 * blocks, 1, most);
-  if (blocks == 1) attend_few_kernel<T, CODE, KV_DIM, 1><<<s.grid, 256, 0, c.stream>>>(a, s.least, s.most);
-  else if (blocks == 2) attend_few_kernel<T, CODE, KV_DIM, 2><<<s.grid, 256, 0, c.stream>>>(a, s.least, s.most);
-  else if constexpr (KV_DIM <= 128) attend_few_kernel<T, CODE, KV_DIM, 4><<<s.grid, 256, 0, c.stream>>>(a, s.least, s.most);
-  join_kernel<T, KV_DIM><<<dim3(s.joins, (s.rows + kJoinRows - 1) / kJoinRows), 64 * kJoinRows, 0, c.stream>>>(a, s.rows, false, s.least, s.most);
+// No block has more than kMinSteps steps, so none is split.
+static bool never_split(const AttendArgs &a) {
+  return (uint64_t)a.max_pages * a.c.page <= (uint64_t)kMinSteps * kStep;
+}
+
+template <int T>
+static void join(const AttendCall &c, const Lists &many, bool with_many, const Lists &few) {
+  if (never_split(c.a)) return;
+  const uint32_t n_many = with_many ? std::min(blocks_bound(c.a, many), c.a.target) : 0;
+  const uint32_t n_few = std::min(blocks_bound(c.a, few), c.a.target);
+  const uint32_t grid = n_many * (kManyBlock / kJoinRows) + n_few * (few.rows / kJoinRows);
+  join_kernel<T, KV_DIM><<<grid, 256, 0, c.stream>>>(c.a, many, n_many, few);
 }
 
 template <int T, int CODE>
 static void launch(const AttendCall &c) {
   const AttendArgs &a = c.a;
-  const uint64_t list = (uint64_t)c.max_new * a.group;
+  const Layout at = layout(c.type, KV_DIM, a.group, c.max_new);
+  const Lists few{1, at.many ? (int64_t)kManyFrom : INT64_MAX, 16 * at.few, at.many ? 2 * a.target * kManyBlock : 0};
+  const uint32_t n_few = blocks_bound(a, few) + a.target;
   if constexpr (T != UZIP_FP32) {
-    if (many_rows(c.type, list)) {
-      const Share s = share_of(a, 128, kManyFrom + 1, INT64_MAX);
-      attend_many_kernel<T, CODE, KV_DIM><<<s.grid, 256, 0, c.stream>>>(a, s.least, s.most);
-      join_kernel<T, KV_DIM><<<dim3(s.joins, (s.rows + kJoinRows - 1) / kJoinRows), 64 * kJoinRows, 0, c.stream>>>(a, s.rows, true, s.least, s.most);
-      launch_few<T, CODE>(c, few_blocks(KV_DIM, a.group), kManyFrom);  // sized for the requests of one token
+    if (at.many) {
+      const Lists many{kManyFrom + 1, INT64_MAX, kManyBlock, 0};
+      const uint32_t n_many = blocks_bound(a, many) + a.target;
+      all_rows_kernel<T, CODE, KV_DIM, 1><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
+      join<T>(c, many, true, few);
       return;
     }
   }
-  launch_few<T, CODE>(c, few_blocks(KV_DIM, list), INT64_MAX);
+  if (at.few == 1) few_rows_kernel<T, CODE, KV_DIM, 1><<<n_few, 256, 0, c.stream>>>(a, few);
+  else if (at.few == 2) few_rows_kernel<T, CODE, KV_DIM, 2><<<n_few, 256, 0, c.stream>>>(a, few);
+  else if constexpr (KV_DIM <= 128) few_rows_kernel<T, CODE, KV_DIM, 4><<<n_few, 256, 0, c.stream>>>(a, few);
+  join<T>(c, few, false, few);
 }
 
 template <>

@@ -8,11 +8,10 @@ torch; every call enqueues on ``stream`` or the current one.
 from __future__ import annotations
 
 import ctypes
-from typing import NamedTuple
 
 import torch
 
-from . import BF16, E4M3FN, E5M2, EINVAL, FP16, FP32, _check, _dev_empty, _lib, _stream
+from . import BF16, E4M3FN, E5M2, EINVAL, FP16, FP32, OK, _check, _dev_empty, _lib, _stream
 
 _c = ctypes
 _vp, _u32, _i64, _sz, _int, _f32 = _c.c_void_p, _c.c_uint32, _c.c_int64, _c.c_size_t, _c.c_int, _c.c_float
@@ -49,10 +48,6 @@ uzip_kv_attend = _lib.uzip_kv_attend
 _TYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
 _CODES = {"e4m3fn": E4M3FN, "e5m2": E5M2, torch.float8_e4m3fn: E4M3FN, torch.float8_e5m2: E5M2,
           E4M3FN: E4M3FN, E5M2: E5M2}
-
-
-def _ptr(x):
-    return x.data_ptr() if x is not None else None
 
 
 def _need(ok: bool, what: str) -> None:
@@ -93,29 +88,45 @@ class KVCache:
                    new(pages, heads), dtype)
 
 
-class KVPlan(NamedTuple):
-    """A step's places, on the GPU (see uzip_kv_plan)."""
-    lens: torch.Tensor      # int32 [requests]
-    q_start: torch.Tensor   # int32 [requests + 1]
-    slots: torch.Tensor     # int64 [rows]
-    runs: torch.Tensor      # int32 [max runs, 2]
-    counts: torch.Tensor    # int32 [2]: pages taken, runs
-    status: torch.Tensor    # int32 [1]
+class KVPlan:
+    """A step's places, on the GPU (see uzip_kv_plan), for up to ``requests`` requests and ``rows`` new tokens: lens
+    int32 [requests], q_start int32 [requests + 1], slots int64 [rows], runs int32 [max runs, 2], counts int32 [2]
+    (pages taken, runs), status int32 [1]."""
+
+    __slots__ = ("requests", "rows", "page_tokens", "lens", "q_start", "slots", "runs", "counts", "status", "_ptrs")
+
+    def __init__(self, requests: int, rows: int, page_tokens: int, device="cuda"):
+        runs = uzip_kv_max_runs(rows, requests, page_tokens) if rows >= 0 and requests >= 0 else 0
+        if runs == 0:
+            _check(EINVAL, "uzip_kv_max_runs")
+
+        def new(*shape, dtype=torch.int32):
+            return torch.empty(*shape, dtype=dtype, device=device)
+        self.requests, self.rows, self.page_tokens = requests, rows, page_tokens
+        self.lens, self.q_start, self.slots = new(requests), new(requests + 1), new(rows, dtype=torch.int64)
+        self.runs, self.counts = new(runs, 2), new(2)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self._ptrs = tuple(t.data_ptr() for t in (self.lens, self.q_start, self.slots, self.runs, self.counts, self.status))
 
 
 def kv_plan_buffers(requests: int, rows: int, page_tokens: int, device="cuda") -> KVPlan:
-    runs = uzip_kv_max_runs(rows, requests, page_tokens)
-    if runs == 0:
-        _check(EINVAL, "uzip_kv_max_runs")
-
-    def new(*shape, dtype=torch.int32):
-        return torch.empty(*shape, dtype=dtype, device=device)
-    return KVPlan(new(requests), new(requests + 1), new(rows, dtype=torch.int64), new(runs, 2), new(2),
-                  torch.zeros(1, dtype=torch.int32, device=device))
+    return KVPlan(requests, rows, page_tokens, device)
 
 
 def _ints(x: torch.Tensor, name: str, dtype=torch.int32) -> None:
-    _need(x.is_cuda and x.dtype == dtype and x.is_contiguous(), f"{name} is a contiguous {dtype} tensor on the GPU")
+    if not (x.is_cuda and x.dtype == dtype and x.is_contiguous()):
+        raise ValueError(f"{name} is a contiguous {dtype} tensor on the GPU")
+
+
+# The current stream's handle without making a Stream object of it, which takes 3 us
+# of a call that takes 4.
+_raw_stream, _device = (getattr(torch._C, name, None) for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+
+
+def _handle(stream) -> int:
+    if stream is not None or _raw_stream is None or _device is None:
+        return _stream(stream)
+    return _raw_stream(_device())
 
 
 def kv_plan(old: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: torch.Tensor, page_tokens: int, rows: int,
@@ -124,19 +135,21 @@ def kv_plan(old: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: tor
     from the front of ``free`` go into ``table`` [requests, max pages].  With
     ``check`` the call waits for the GPU and raises UzipError where a request
     took no part."""
-    for x, name in ((old, "old"), (new, "new"), (free, "free"), (table, "table")):
-        _ints(x, name)
+    _ints(old, "old")
+    _ints(new, "new")
+    _ints(free, "free")
+    _ints(table, "table")
     n = old.numel()
-    _need(new.numel() == n and table.dim() == 2 and table.shape[0] == n, "old, new and table are of one batch")
+    if new.numel() != n or table.dim() != 2 or table.shape[0] != n:
+        raise ValueError("old, new and table are of one batch")
     if out is None:
-        out = kv_plan_buffers(n, rows, page_tokens, old.device)
-    else:
-        _need(out.lens.numel() >= n and out.q_start.numel() > n and out.slots.numel() >= rows and
-              out.runs.shape[0] >= uzip_kv_max_runs(rows, n, page_tokens), "out holds fewer requests or rows")
-    _check(uzip_kv_plan(old.data_ptr(), new.data_ptr(), n, free.data_ptr(), free.numel(), page_tokens, rows,
-                        table.data_ptr(), table.shape[1], out.lens.data_ptr(), out.q_start.data_ptr(),
-                        out.slots.data_ptr(), out.runs.data_ptr(), out.counts.data_ptr(), out.status.data_ptr(),
-                        _stream(stream)), "uzip_kv_plan")
+        out = KVPlan(n, rows, page_tokens, old.device)
+    elif n > out.requests or not 0 <= rows <= out.rows or page_tokens < out.page_tokens:
+        raise ValueError("out is for fewer requests or rows, or larger pages")
+    rc = uzip_kv_plan(old.data_ptr(), new.data_ptr(), n, free.data_ptr(), free.numel(), page_tokens, rows, table.data_ptr(),
+                      table.shape[1], *out._ptrs, _handle(stream))
+    if rc != OK:
+        _check(rc, "uzip_kv_plan")
     if check:
         (stream or torch.cuda.current_stream(old.device)).synchronize()
         _check(int(out.status.item()), "uzip_kv_plan")
@@ -144,24 +157,28 @@ def kv_plan(old: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: tor
 
 
 def _rows(x: torch.Tensor, name: str, dim: int) -> int:
-    _need(x.is_cuda and x.dim() == 3 and x.dtype in _TYPES and x.shape[2] == dim and (x.stride(2) == 1 or x.numel() == 0),
-          f"{name} is [rows, heads, {dim}] in bf16, fp16 or fp32 with each head's values side by side")
-    return _TYPES[x.dtype]
+    t = _TYPES.get(x.dtype)
+    if t is None or not x.is_cuda or x.dim() != 3 or x.shape[2] != dim or (x.stride(2) != 1 and x.numel()):
+        raise ValueError(f"{name} is [rows, heads, {dim}] in bf16, fp16 or fp32 with each head's values side by side")
+    return t
 
 
 def kv_store(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, runs: torch.Tensor,
              counts: torch.Tensor, stream=None) -> None:
     """Write rows of k and v [rows, heads, dim] to the places that kv_plan made."""
     t = _rows(k, "k", cache.dim)
-    _need(_rows(v, "v", cache.dim) == t and k.shape == v.shape and k.shape[1] == cache.heads, "k and v are alike")
+    if _rows(v, "v", cache.dim) != t or k.shape != v.shape or k.shape[1] != cache.heads:
+        raise ValueError("k and v are [rows, the cache's heads, dim] of one type")
     _ints(slots, "slots", torch.int64)
     _ints(runs, "runs")
     _ints(counts, "counts")
     rows = k.shape[0]
-    _need(slots.numel() >= rows and counts.numel() >= 2, "slots has an entry for each row")
-    _check(uzip_kv_store(cache, t, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), rows,
-                         slots.data_ptr(), runs.data_ptr(), counts.data_ptr(), runs.shape[0], _stream(stream)),
-           "uzip_kv_store")
+    if slots.numel() < rows or counts.numel() < 2 or runs.numel() != 2 * runs.shape[0]:
+        raise ValueError("slots has an entry for each row, runs two for each run, counts two")
+    rc = uzip_kv_store(cache, t, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), rows,
+                       slots.data_ptr(), runs.data_ptr(), counts.data_ptr(), runs.shape[0], _handle(stream))
+    if rc != OK:
+        _check(rc, "uzip_kv_store")
 
 
 def kv_attend_workspace(q: torch.Tensor, cache: KVCache, requests: int, max_new: int) -> torch.Tensor:
@@ -180,25 +197,27 @@ def kv_attend(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: torch.
     t = _rows(q, "q", cache.dim)
     rows, heads = q.shape[0], q.shape[1]
     n = lens.numel()
-    _need(0 <= window < 1 << 32 and 0 <= max_new < 1 << 32, "window and max_new are not negative")
     _ints(table, "table")
     _ints(lens, "lens")
     _ints(q_start, "q_start")
-    _need(table.dim() == 2 and table.shape[0] >= n and q_start.numel() > n, "table, lens and q_start are of one batch")
+    if table.dim() != 2 or table.shape[0] < n or q_start.numel() <= n:
+        raise ValueError("table, lens and q_start are of one batch")
+    if not (0 <= window < 1 << 32 and 0 <= max_new < 1 << 32):
+        raise ValueError("window and max_new are not negative")
     if out is None:
         out = torch.empty(rows, heads, cache.dim, dtype=q.dtype, device=q.device)
-    else:
-        _need(_rows(out, "out", cache.dim) == t and out.shape == q.shape, "out is like q")
+    elif _rows(out, "out", cache.dim) != t or out.shape != q.shape:
+        raise ValueError("out is like q")
     if lse is None:
         lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device)
-    else:
-        _need(lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2],
-              "lse is fp32 [rows, query heads]")
+    elif not (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]):
+        raise ValueError("lse is fp32 [rows, query heads]")
     if ws is None:
         ws = kv_attend_workspace(q, cache, n, max_new)
-    _check(uzip_kv_attend(cache, t, q.data_ptr(), q.stride(0), q.stride(1), rows, heads, table.data_ptr(), table.shape[1],
-                          lens.data_ptr(), q_start.data_ptr(), n, max_new,
-                          cache.dim ** -0.5 if scale is None else scale, window, out.data_ptr(), out.stride(0),
-                          out.stride(1), lse.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)),
-           "uzip_kv_attend")
+    rc = uzip_kv_attend(cache, t, q.data_ptr(), q.stride(0), q.stride(1), rows, heads, table.data_ptr(), table.shape[1],
+                        lens.data_ptr(), q_start.data_ptr(), n, max_new, cache.dim ** -0.5 if scale is None else scale, window,
+                        out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(), ws.data_ptr(),
+                        ws.numel() * ws.element_size(), _handle(stream))
+    if rc != OK:
+        _check(rc, "uzip_kv_attend")
     return out, lse
