@@ -16,6 +16,10 @@ struct Cache {
   uint32_t n_pages, heads, dim, page, page_shift;
 };
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // ---- 8-bit codes ----
 // E4M3: 1.75 * 2^8 is the largest value; E5M2: 1.75 * 2^15.  An exponent byte e
 // scales a page by 2^(e - 127).  e >= 27 keeps every scaled code a normal
@@ -57,6 +61,18 @@ __device__ __forceinline__ uint32_t encode(float x, float inv) {
   const uint32_t c = CODE == UZIP_E4M3FN ? (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false)
                                          : (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(y, y, 0, false);
   return c & 0xFFu;
+}
+
+// Four codes of finite x * inv within the codes' range, x[0]'s in the low byte.
+template <int CODE>
+__device__ __forceinline__ uint32_t encode4(const float *x, float inv) {
+  if constexpr (CODE == UZIP_E4M3FN) {
+    const int c = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, c, true);
+  } else {
+    const int c = __builtin_amdgcn_cvt_pk_bf8_f32(x[0] * inv, x[1] * inv, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(x[2] * inv, x[3] * inv, c, true);
+  }
 }
 
 // The value of a code (byte 0 of c).
