@@ -30,7 +30,7 @@ struct AttendArgs {
   float *part_acc;   // [row][dim]: acc of pieces that are joined, a row for each of their blocks' rows
   float *part_ml;    // [row][2]: their m and l
   uint32_t n_rows, n_q_heads, group, max_pages, n_reqs, window;
-  uint32_t target;   // pieces that fill the GPU
+  uint32_t units;    // compute units
   float scale_log2;  // |scale| log2 e
   bool negate;       // scale < 0: the queries change sign instead
   bool q_vec, out_vec;  // rows start at multiples of 16 (q) and 4 elements (out), so loads and stores may be wide
@@ -42,15 +42,17 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStep = 64;      // tokens of a step
-constexpr int kMinSteps = 4;   // steps of a piece, so each of a workgroup's waves has one
+constexpr int kMinSteps = 8;   // steps of a piece: two for each of a workgroup's waves
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
-// Lists of more rows than this go to the many-rows kernel, in blocks of 128 (fp32
-// has none: its three terms make the matrix units the bound, which few rows reach
-// as well).
-constexpr uint32_t kManyFrom = 64, kManyBlock = 128;
+// Lists of more rows than this go to the many-rows kernel, in blocks of 128 (32
+// requests of 1000 to 4000 tokens, 48 rows of dim 128: 100 us, by 16 x 3 or 64 rows at
+// a time 123; 36 rows of dim 256: 97 us, by 32 rows 66).  fp32 has none: its three terms
+// make the matrix units the bound, which few rows reach as well.
+constexpr uint32_t many_from(uint32_t dim) { return dim <= 128 ? 32 : 64; }
+constexpr uint32_t kManyBlock = 128;
 
 // ------------------------------------------------------------------ pieces of work
 struct Request {
@@ -95,6 +97,7 @@ struct Lists {
   int64_t least, most;
   uint32_t rows;
   uint32_t slots;  // first row of the workspace for their pieces
+  bool many;       // the many-rows kernel's
 };
 
 struct Piece {
@@ -125,34 +128,67 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
   return x;
 }
 
-// Which piece of the lists is number `index`, found by the whole workgroup.  All blocks'
-// steps are shared out so that about `target` pieces of equal length come of
-// them; a block shorter than that stays whole.  With JOIN the index counts the
-// blocks that were split instead.  At most target + blocks pieces, at most
-// target split blocks, and at most 2 target slots come of it: a block of n
-// steps is split only where n > S, the steps of a piece, into ceil(n / S) <
-// 2 n / S.  Every workgroup sums over the requests for itself: two scans.
+// How many steps make a piece, from the steps and blocks of all lists.
+//
+// Many rows: two pieces for each compute unit.
+// Few rows: where there are fewer blocks than compute units, so that about one piece
+// comes to each (steps / S + blocks / 2 pieces come of S): one round of longer pieces
+// beats two of shorter ones, a piece's beginning and end being a few us (a request of
+// 100000 tokens, 8 heads: 49 us, with two to a unit 56; 8 requests of 2000 to 4000
+// tokens 22.5 and 29.6).  Where there are more, pieces of no less than 32 steps and up
+// to four to a unit, which even out requests of unlike lengths (64 requests of 1 to
+// 8000 tokens: 114 us, with one to a unit 130).
+constexpr uint32_t kFewPieces = 4, kManyPieces = 2, kLongPiece = 32;
+__device__ __forceinline__ uint64_t piece_steps(const AttendArgs &a, bool many, uint64_t steps, uint64_t blocks) {
+  const uint64_t units = a.units;
+  if (!many && blocks >= units) return max((steps + kFewPieces * units - 1) / (kFewPieces * units), (uint64_t)kLongPiece);
+  const uint64_t pieces = many ? kManyPieces * units : units - blocks / 2;
+  return max((steps + pieces - 1) / pieces, (uint64_t)kMinSteps);
+}
+
+// Which piece of the lists is number `index`, found by the whole workgroup.  A block
+// of n steps is split only where n > S = piece_steps, into ceil(n / S) < 2 n / S pieces:
+// with at most k units of pieces' worth of steps, k = kFewPieces or kManyPieces, there are at
+// most k units + blocks pieces, k units split blocks and 2 k units slots of the
+// workspace.  With JOIN the index counts the blocks that were split instead.  Every
+// workgroup sums over the requests for itself: two scans.
 template <int THREADS, bool JOIN>
 __device__ bool find_piece(const AttendArgs &a, const Lists &lists, uint32_t index, Piece *out) {
   constexpr int kWaves = THREADS / 64;
   const uint32_t rows = lists.rows;
-  __shared__ uint64_t part[2 * kWaves];
+  __shared__ uint64_t part[3 * kWaves];
   __shared__ Piece found;
   const uint32_t tid = threadIdx.x, wave = tid >> 6, n = a.n_reqs + 1;  // with the rows of no request
   const uint32_t each = (n + THREADS - 1) / THREADS, lo = min(n, tid * each), hi = min(n, lo + each);
-  uint64_t steps = 0;
+  // each thread's first request, most often its only one, is looked up once
+  const Request first = lo < hi ? request(a, lo) : Request{};
+  auto request_at = [&](uint32_t i) { return i == lo ? first : request(a, i); };
+  uint64_t steps = 0, blocks = 0;
   for (uint32_t i = lo; i < hi; ++i) {
-    const Request q = request(a, i);
-    steps += (uint64_t)blocks_of(a, q, lists) * steps_of(a, q, rows);
+    const Request q = request_at(i);
+    const uint64_t b = blocks_of(a, q, lists);
+    blocks += b;
+    steps += b * steps_of(a, q, rows);
   }
-  steps = wave_scan64(steps);
-  if ((tid & 63) == 63) part[wave] = steps;
-  __syncthreads();
-  uint64_t all = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) all += part[w];
-  all *= a.c.heads;
-  const uint64_t length = max((all + a.target - 1) / a.target, (uint64_t)kMinSteps);  // S
+  for (int o = 32; o; o >>= 1) {
+    steps += __shfl_xor(steps, o);
+    blocks += __shfl_xor(blocks, o);
+  }
+  if ((tid & 63) == 0) {
+    part[wave] = steps;
+    part[kWaves + wave] = blocks;
+  }
+  __syncthreads();
+  steps = blocks = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    steps += part[w];
+    blocks += part[kWaves + w];
+  }
+  steps *= a.c.heads;
+  blocks *= a.c.heads;
+  const uint64_t length = piece_steps(a, lists.many, steps, blocks);
   auto count = [&](const Request &q, uint32_t *splits) {
     const uint32_t b = blocks_of(a, q, lists);
     *splits = (uint32_t)max((steps_of(a, q, rows) + length - 1) / length, (uint64_t)1);
@@ -161,19 +197,19 @@ __device__ bool find_piece(const AttendArgs &a, const Lists &lists, uint32_t ind
   };
   uint64_t mine = 0;
   uint32_t splits;
-  for (uint32_t i = lo; i < hi; ++i) mine += count(request(a, i), &splits);
+  for (uint32_t i = lo; i < hi; ++i) mine += count(request_at(i), &splits);
   const uint64_t incl = wave_scan64(mine);
-  if ((tid & 63) == 63) part[kWaves + wave] = incl;
+  if ((tid & 63) == 63) part[2 * kWaves + wave] = incl;
   __syncthreads();
   uint64_t at = incl - mine, total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    if (w < (int)wave) at += part[kWaves + w];
-    total += part[kWaves + w];
+    if (w < (int)wave) at += part[2 * kWaves + w];
+    total += part[2 * kWaves + w];
   }
   if (index >= (uint32_t)total) return false;
   for (uint32_t i = lo; i < hi; ++i) {
-    const Request q = request(a, i);
+    const Request q = request_at(i);
     const uint64_t c = count(q, &splits);
     const uint32_t rest = index - (uint32_t)at;
     if (index >= (uint32_t)at && rest < (uint32_t)c) {
@@ -380,7 +416,7 @@ __device__ __forceinline__ Frag class_frag(uint32_t lo, uint32_t hi, int kind) {
 __device__ __forceinline__ float class_value(int kind) { return kind == 0 ? NAN : kind == 1 ? INFINITY : -INFINITY; }
 
 // ------------------------------------------------------------------ few rows
-// One workgroup for up to 16 NM rows and a piece of their tokens, one wave a
+// One workgroup for up to 16 NM rows (NM 1 or 2) and a piece of their tokens, one wave a
 // step of 64 tokens, everything from memory straight into registers:
 //   S^T = K Q^T, four tiles of 16 tokens: row m of tile i is token 16 (m / 4) + 4
 //   i + m % 4, so that a lane ends up with the scores of 16 tokens in a row for one
@@ -1103,23 +1139,17 @@ struct AttendCall {
   uint32_t max_new;
   hipStream_t stream;
 };
-// Blocks of 16 rows that a workgroup of the few-rows kernel takes at once, for lists
-// of `list` rows.
-constexpr uint32_t few_blocks(uint32_t dim, uint64_t list) {
-  const uint32_t most = dim <= 128 ? 4 : 2;  // LDS: 16 NM rows of dim fp32 values, twice, in 64 KiB
-  return list <= 16 ? 1 : list <= 32 || most == 2 ? 2 : 4;
-}
 // What a call launches and where its pieces go.
 struct Layout {
   bool many;              // the kernel for both, with blocks of 16 rows for the short lists
   uint32_t few;           // blocks of 16 rows to a workgroup
-  uint64_t rows_for_one;  // workspace rows for each slot of the target's 2 * target
+  uint64_t rows_for_one;  // workspace rows for each compute unit
 };
 inline Layout layout(uzip_dtype type, uint32_t dim, uint32_t group, uint32_t max_new) {
   const uint64_t list = (uint64_t)max_new * group;
-  const bool many = type != UZIP_FP32 && list > kManyFrom;
-  const uint32_t few = many ? 1 : few_blocks(dim, list);
-  return {many, few, (many ? kManyBlock : 0) + 16ull * few};
+  const bool many = type != UZIP_FP32 && list > many_from(dim);
+  const uint32_t few = many || list <= 16 ? 1 : 2;
+  return {many, few, 2 * (many ? kManyPieces * kManyBlock : 0) + 2 * kFewPieces * 16ull * few};
 }
 template <int D>
 uzip_status launch_attend(const AttendCall &call);

@@ -8,9 +8,7 @@
 namespace uzip_kv {
 namespace {
 
-// Pieces of work that fill the GPU: two workgroups for each compute unit.
-uint32_t target_pieces(int cus) { return 2u * (uint32_t)std::max(cus, 1); }
-constexpr uint32_t kMostTarget = 512;  // what the workspace is sized for, whatever the device
+constexpr uint32_t kMostUnits = 256;  // compute units that the workspace is sized for, whatever the device
 
 bool attend_sizes(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_heads, uint32_t n_heads, uint32_t head_dim,
                   uint32_t n_reqs) {
@@ -30,7 +28,7 @@ size_t uzip_kv_attend_workspace(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_
                                 uint32_t head_dim, uint32_t n_reqs, uint32_t max_new) {
   if (!attend_sizes(dtype, n_rows, n_q_heads, n_heads, head_dim, n_reqs)) return 0;
   const Layout at = layout(dtype, head_dim, n_q_heads / n_heads, max_new);
-  return (size_t)(2 * kMostTarget * at.rows_for_one * (head_dim + 2) * sizeof(float));
+  return (size_t)(kMostUnits * at.rows_for_one * (head_dim + 2) * sizeof(float));
 }
 
 uzip_status uzip_kv_attend(const uzip_kv_cache *cache, uzip_dtype dtype, const void *d_q, int64_t q_row,
@@ -72,7 +70,7 @@ uzip_status uzip_kv_attend(const uzip_kv_cache *cache, uzip_dtype dtype, const v
   a.max_pages = max_pages;
   a.n_reqs = n_reqs;
   a.window = window;
-  a.target = std::min(target_pieces(cus), kMostTarget);
+  a.units = std::min((uint32_t)std::max(cus, 1), kMostUnits);
   a.scale_log2 = std::fabs(scale) * 1.4426950408889634f;
   a.negate = scale < 0;
   auto at_multiples = [&](const void *p, int64_t row, int64_t head, int64_t of) {
@@ -81,7 +79,7 @@ uzip_status uzip_kv_attend(const uzip_kv_cache *cache, uzip_dtype dtype, const v
   a.q_vec = at_multiples(d_q, q_row, q_head, 16);
   a.out_vec = at_multiples(d_out, out_row, out_head, 4 * bytes);
   a.part_acc = (float *)d_ws;
-  a.part_ml = a.part_acc + 2ull * kMostTarget * layout(dtype, cache->head_dim, a.group, max_new).rows_for_one * cache->head_dim;
+  a.part_ml = a.part_acc + (size_t)kMostUnits * layout(dtype, cache->head_dim, a.group, max_new).rows_for_one * cache->head_dim;
   call.type = dtype;
   call.code = cache->dtype;
   call.max_new = max_new;

@@ -7,12 +7,20 @@
 
 namespace uzip_kv {
 
-// At most how many pieces, and how many split blocks, find_piece makes of the lists.
+// At most how many blocks the lists have, how many of them are split, and how many
+// pieces there are.
 static uint32_t blocks_bound(const AttendArgs &a, const Lists &l) {
   // full blocks and a last one for each list, or what lists of l.most rows can have
   const uint64_t lists = a.n_reqs + 1, all = (uint64_t)a.n_rows * a.group;
   const uint64_t each = l.most < (int64_t)all ? ((uint64_t)l.most + l.rows - 1) / l.rows : UINT32_MAX;
   return (uint32_t)(a.c.heads * std::min(all / l.rows + lists, lists * each));
+}
+
+static uint32_t most_split(const AttendArgs &a, const Lists &l) {
+  return std::min(blocks_bound(a, l), (l.many ? kManyPieces : kFewPieces) * a.units);
+}
+static uint32_t most_pieces(const AttendArgs &a, const Lists &l) {
+  return blocks_bound(a, l) + (l.many ? kManyPieces : kFewPieces) * a.units;
 }
 
 // No block has more than kMinSteps steps, so none is split.
@@ -23,8 +31,7 @@ static bool never_split(const AttendArgs &a) {
 template <int T>
 static void join(const AttendCall &c, const Lists &many, bool with_many, const Lists &few) {
   if (never_split(c.a)) return;
-  const uint32_t n_many = with_many ? std::min(blocks_bound(c.a, many), c.a.target) : 0;
-  const uint32_t n_few = std::min(blocks_bound(c.a, few), c.a.target);
+  const uint32_t n_many = with_many ? most_split(c.a, many) : 0, n_few = most_split(c.a, few);
   const uint32_t grid = n_many * (kManyBlock / kJoinRows) + n_few * (few.rows / kJoinRows);
   join_kernel<T, KV_DIM><<<grid, 256, 0, c.stream>>>(c.a, many, n_many, few);
 }
@@ -33,20 +40,19 @@ template <int T, int CODE>
 static void launch(const AttendCall &c) {
   const AttendArgs &a = c.a;
   const Layout at = layout(c.type, KV_DIM, a.group, c.max_new);
-  const Lists few{1, at.many ? (int64_t)kManyFrom : INT64_MAX, 16 * at.few, at.many ? 2 * a.target * kManyBlock : 0};
-  const uint32_t n_few = blocks_bound(a, few) + a.target;
+  const Lists few{1, at.many ? (int64_t)many_from(KV_DIM) : INT64_MAX, 16 * at.few, at.many ? 2 * kManyPieces * a.units * kManyBlock : 0, false};
+  const uint32_t n_few = most_pieces(a, few);
   if constexpr (T != UZIP_FP32) {
     if (at.many) {
-      const Lists many{kManyFrom + 1, INT64_MAX, kManyBlock, 0};
-      const uint32_t n_many = blocks_bound(a, many) + a.target;
+      const Lists many{many_from(KV_DIM) + 1, INT64_MAX, kManyBlock, 0, true};
+      const uint32_t n_many = most_pieces(a, many);
       all_rows_kernel<T, CODE, KV_DIM, 1><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
       join<T>(c, many, true, few);
       return;
     }
   }
   if (at.few == 1) few_rows_kernel<T, CODE, KV_DIM, 1><<<n_few, 256, 0, c.stream>>>(a, few);
-  else if (at.few == 2) few_rows_kernel<T, CODE, KV_DIM, 2><<<n_few, 256, 0, c.stream>>>(a, few);
-  else if constexpr (KV_DIM <= 128) few_rows_kernel<T, CODE, KV_DIM, 4><<<n_few, 256, 0, c.stream>>>(a, few);
+  else few_rows_kernel<T, CODE, KV_DIM, 2><<<n_few, 256, 0, c.stream>>>(a, few);
   join<T>(c, few, false, few);
 }
 
