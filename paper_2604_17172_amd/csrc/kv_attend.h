@@ -94,8 +94,8 @@ __device__ __forceinline__ bool sees(const Seen &s, int32_t t) { return (uint32_
 
 // The lists that one kernel takes: those of least to most rows, in blocks of rows.
 struct Lists {
-  int64_t least, most;
-  uint32_t rows;
+  uint32_t least, most;
+  uint32_t rows, shift;  // rows = 2^shift
   uint32_t slots;  // first row of the workspace for their pieces
   bool many;       // the many-rows kernel's
 };
@@ -108,15 +108,15 @@ struct Piece {
 };
 
 __device__ __forceinline__ uint32_t blocks_of(const AttendArgs &a, const Request &q, const Lists &l) {
-  const int64_t list = (int64_t)q.rows * a.group;
-  return list >= l.least && list <= l.most ? (uint32_t)((list + l.rows - 1) / l.rows) : 0u;
+  const uint32_t list = (uint32_t)q.rows * a.group;  // at most UZIP_KV_MAX_ROW_HEADS
+  return list >= l.least && list <= l.most ? (list + l.rows - 1) >> l.shift : 0u;
 }
 
 // The most steps that a block of `rows` rows of the request can have.
 __device__ __forceinline__ uint32_t steps_of(const AttendArgs &a, const Request &q, uint32_t rows) {
-  int64_t tokens = q.len;
-  if (a.window) tokens = min(tokens, (int64_t)a.window + rows / a.group + 1 + kStep);
-  return (uint32_t)((tokens + kStep - 1) / kStep);
+  uint32_t tokens = (uint32_t)q.len;
+  if (a.window) tokens = min(tokens, min(a.window, (uint32_t)INT32_MAX) + rows + kStep);
+  return (tokens + kStep - 1) / kStep;
 }
 
 __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
@@ -139,11 +139,12 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
 // to four to a unit, which even out requests of unlike lengths (64 requests of 1 to
 // 8000 tokens: 114 us, with one to a unit 130).
 constexpr uint32_t kFewPieces = 4, kManyPieces = 2, kLongPiece = 32;
-__device__ __forceinline__ uint64_t piece_steps(const AttendArgs &a, bool many, uint64_t steps, uint64_t blocks) {
-  const uint64_t units = a.units;
-  if (!many && blocks >= units) return max((steps + kFewPieces * units - 1) / (kFewPieces * units), (uint64_t)kLongPiece);
-  const uint64_t pieces = many ? kManyPieces * units : units - blocks / 2;
-  return max((steps + pieces - 1) / pieces, (uint64_t)kMinSteps);
+__device__ __forceinline__ uint32_t piece_steps(const AttendArgs &a, bool many, uint64_t steps, uint64_t blocks) {
+  const bool few_blocks = !many && blocks < a.units;
+  const uint32_t pieces = many ? kManyPieces * a.units : few_blocks ? a.units - (uint32_t)blocks / 2 : kFewPieces * a.units;
+  const uint32_t least = many || few_blocks ? kMinSteps : kLongPiece;
+  if (steps <= (uint64_t)least * pieces) return least;
+  return (uint32_t)min((steps + pieces - 1) / pieces, (uint64_t)INT32_MAX);
 }
 
 // Which piece of the lists is number `index`, found by the whole workgroup.  A block
@@ -188,10 +189,11 @@ __device__ bool find_piece(const AttendArgs &a, const Lists &lists, uint32_t ind
   }
   steps *= a.c.heads;
   blocks *= a.c.heads;
-  const uint64_t length = piece_steps(a, lists.many, steps, blocks);
+  const uint32_t length = piece_steps(a, lists.many, steps, blocks);
   auto count = [&](const Request &q, uint32_t *splits) {
     const uint32_t b = blocks_of(a, q, lists);
-    *splits = (uint32_t)max((steps_of(a, q, rows) + length - 1) / length, (uint64_t)1);
+    const uint32_t n = steps_of(a, q, rows);
+    *splits = n > length ? (n + length - 1) / length : 1u;
     const uint64_t pieces = (uint64_t)b * a.c.heads * (JOIN ? (*splits > 1 ? 1u : 0u) : *splits);
     return pieces | (*splits > 1 ? (uint64_t)b * a.c.heads * *splits : 0) << 32;  // pieces; slots
   };

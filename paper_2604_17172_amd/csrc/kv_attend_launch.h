@@ -12,7 +12,7 @@ namespace uzip_kv {
 static uint32_t blocks_bound(const AttendArgs &a, const Lists &l) {
   // full blocks and a last one for each list, or what lists of l.most rows can have
   const uint64_t lists = a.n_reqs + 1, all = (uint64_t)a.n_rows * a.group;
-  const uint64_t each = l.most < (int64_t)all ? ((uint64_t)l.most + l.rows - 1) / l.rows : UINT32_MAX;
+  const uint64_t each = l.most < all ? ((uint64_t)l.most + l.rows - 1) / l.rows : UINT32_MAX;
   return (uint32_t)(a.c.heads * std::min(all / l.rows + lists, lists * each));
 }
 
@@ -40,11 +40,11 @@ template <int T, int CODE>
 static void launch(const AttendCall &c) {
   const AttendArgs &a = c.a;
   const Layout at = layout(c.type, KV_DIM, a.group, c.max_new);
-  const Lists few{1, at.many ? (int64_t)many_from(KV_DIM) : INT64_MAX, 16 * at.few, at.many ? 2 * kManyPieces * a.units * kManyBlock : 0, false};
+  const Lists few{1, at.many ? many_from(KV_DIM) : UINT32_MAX, 16 * at.few, at.few == 1 ? 4u : 5u, at.many ? 2 * kManyPieces * a.units * kManyBlock : 0, false};
   const uint32_t n_few = most_pieces(a, few);
   if constexpr (T != UZIP_FP32) {
     if (at.many) {
-      const Lists many{many_from(KV_DIM) + 1, INT64_MAX, kManyBlock, 0, true};
+      const Lists many{many_from(KV_DIM) + 1, UINT32_MAX, kManyBlock, 7, 0, true};
       const uint32_t n_many = most_pieces(a, many);
       all_rows_kernel<T, CODE, KV_DIM, 1><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
       join<T>(c, many, true, few);
