@@ -1116,8 +1116,13 @@ __device__ void join_rows(const AttendArgs &a, const Lists &lists, bool last_fir
 }
 
 // ------------------------------------------------------------------ kernels
+// Two workgroups to a compute unit where at most a few registers spill for it (32
+// requests, 20 rows of dim 128: 47 us, one to a unit 59; one row of dim 192: 50 and 55;
+// but of dim 256: 35 and 27).
+template <int T, int D, int NM>
+constexpr int kFewPerUnit = (D <= 128 ? T != UZIP_FP32 || NM == 1 : D == 192 && NM == 1 && T != UZIP_FP32) ? 2 : 1;
 template <int T, int CODE, int D, int NM>
-__global__ __launch_bounds__(256) void few_rows_kernel(AttendArgs a, Lists few) {
+__global__ __launch_bounds__(256, (kFewPerUnit<T, D, NM>)) void few_rows_kernel(AttendArgs a, Lists few) {
   few_rows<T, CODE, D, NM>(a, few, blockIdx.x);
 }
 // Long lists and short ones in one launch: the first workgroups take the pieces of

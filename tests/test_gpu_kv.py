@@ -335,6 +335,24 @@ def test_attend(uz, case):
     attend_case(uz, *args, **more)
 
 
+def test_attend_many_requests(uz):
+    """More requests than a workgroup has threads, single tokens and pieces of prompts among them."""
+    say("many requests")
+    g = np.random.default_rng(81)
+    n = 700
+    ctx, new = g.integers(0, 60, n), np.where(g.random(n) < 0.03, 40, g.integers(0, 3, n))
+    attend_case(uz, 16, 64, 1, 2, "bf16", "e4m3fn", ctx.tolist(), new.tolist())
+    attend_case(uz, 32, 64, 1, 3, "fp16", "e5m2", ctx.tolist(), np.minimum(new, 2).tolist(), window=19)
+
+
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("rows", [15, 17, 31, 33, 65, 130])
+def test_attend_on_both_sides_of_the_kernels_lines(uz, dim, kind, rows):
+    """Lists of 16, 32 and 64 rows are where kernels change; a block has 16, 32 or 128."""
+    attend_case(uz, 64, dim, 1, 1, kind, "e4m3fn", [700, 3], [rows, 1], fused=1)
+
+
 @pytest.mark.parametrize("kind,dim,ctx", [("bf16", 128, 5000), ("fp16", 64, 4097), ("fp32", 96, 3333)])
 def test_attend_long_contexts_are_split_and_joined(uz, kind, dim, ctx):
     say("long", kind, dim, ctx)
@@ -585,3 +603,14 @@ def test_refusals_of_the_wrappers(uz):
         uz.kv_plan(n, n, n, t, 16, 100, out=plan)
     with pytest.raises(uz.UzipError):
         uz.kv_plan(n, n, n, t, 17, 2, out=None)
+
+
+def test_handoff_example():
+    """Plan, store, attend and the codec together: a cache handed over answers as the one that stayed, bit for bit."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "kv_handoff.py")
+    spec = importlib.util.spec_from_file_location("kv_handoff", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    assert mod.main(prompts=(130, 1, 300), answer=70) == 0
