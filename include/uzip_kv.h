@@ -34,7 +34,8 @@
  *     and runs on the device hold.  A page number outside [0, n_pages) is no
  *     page: nothing is stored to it and its tokens are not attended to.
  *   - A call keeps nothing for later calls; the results are the same bits
- *     whatever else runs on the GPU.
+ *     whatever else runs on the GPU.  Calls that overlap in time need separate
+ *     workspaces.
  */
 #ifndef UZIP_KV_H
 #define UZIP_KV_H
@@ -60,7 +61,7 @@ typedef struct {
 /* Requests of one plan, and rows of one call. */
 #define UZIP_KV_MAX_REQUESTS 4096
 #define UZIP_KV_MAX_ROWS (1u << 22)
-#define UZIP_KV_MAX_ROW_HEADS (1u << 27) /* rows times query heads of one uzip_kv_attend */
+#define UZIP_KV_MAX_ROW_HEADS (1u << 26) /* rows times query heads of one uzip_kv_attend */
 
 /* Entries of d_runs: the most runs that n_rows new tokens of n_reqs requests
  * can make, at least 1.  Returns 0 for invalid arguments. */
@@ -89,7 +90,8 @@ uint32_t uzip_kv_max_runs(uint32_t n_rows, uint32_t n_reqs, uint32_t page_tokens
  * rows do not fit n_rows (UZIP_EINVAL) takes no part: d_lens reads 0, its slots
  * -1, its table stays, and so it is with every later request that needs a page
  * once d_free is at its end.  If both errors occur the status is UZIP_ENOSPC.
- * n_reqs <= UZIP_KV_MAX_REQUESTS.  Errors: EINVAL, EHIP, EUNSUPPORTED. */
+ * The outputs are other arrays than d_old and d_new (EINVAL where d_lens is one of
+ * them).  n_reqs <= UZIP_KV_MAX_REQUESTS.  Errors: EINVAL, EHIP, EUNSUPPORTED. */
 uzip_status uzip_kv_plan(const int32_t *d_old, const int32_t *d_new, uint32_t n_reqs, const int32_t *d_free,
                          uint32_t n_free, uint32_t page_tokens, uint32_t n_rows, int32_t *d_table,
                          uint32_t max_pages, int32_t *d_lens, int32_t *d_q_start, int64_t *d_slots,
@@ -130,7 +132,7 @@ size_t uzip_kv_attend_workspace(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_
  * 32 bits; probabilities enter the second product with at least 8 bits for
  * bf16, 16 for fp16 and 24 for fp32.
  *   max_new:     the most new tokens of a request.  It chooses kernels: a wrong
- *                value costs time only.
+ *                value costs time, and the last bits may differ.
  *   d_table, max_pages, d_lens, d_q_start, n_reqs: as uzip_kv_plan leaves them; a
  *                length past max_pages * P counts as that.
  *   d_out:       row r, head a at d_out + r * out_row + a * out_head (elements).

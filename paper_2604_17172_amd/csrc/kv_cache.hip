@@ -532,6 +532,7 @@ uzip_status uzip_kv_plan(const int32_t *d_old, const int32_t *d_new, uint32_t n_
                         (const void *)d_status})
     if (!aligned(p, 4)) return UZIP_EINVAL;
   if (!aligned(d_slots, 8)) return UZIP_EINVAL;
+  if (n_reqs && (d_lens == d_old || d_lens == d_new)) return UZIP_EINVAL;
   if (const uzip_status s = device(nullptr); s != UZIP_OK) return s;
   PlanArgs a{d_old, d_new, d_free, d_table, d_lens, d_q_start, d_runs, d_counts, d_slots, (int *)d_status,
              n_reqs, n_free, (uint32_t)__builtin_ctz(page_tokens), n_rows, max_pages};

@@ -7,6 +7,7 @@ torch; every call enqueues on ``stream`` or the current one.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import torch
@@ -74,7 +75,7 @@ class KVCache:
         _need(dtype in _CODES, "dtype is e4m3fn or e5m2")
         self.k, self.k_exp, self.v, self.v_exp = k, k_exp, v, v_exp
         self.pages, self.heads, self.page_tokens, self.dim = pages, heads, page, dim
-        self.code, self.device = _CODES[dtype], k.device
+        self.code, self.device, self.index = _CODES[dtype], k.device, k.get_device()
         self.desc = uzip_kv_cache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), pages, heads, dim, page,
                                   self.code)
         self._as_parameter_ = _c.byref(self.desc)
@@ -113,20 +114,24 @@ def kv_plan_buffers(requests: int, rows: int, page_tokens: int, device="cuda") -
     return KVPlan(requests, rows, page_tokens, device)
 
 
-def _ints(x: torch.Tensor, name: str, dtype=torch.int32) -> None:
-    if not (x.is_cuda and x.dtype == dtype and x.is_contiguous()):
-        raise ValueError(f"{name} is a contiguous {dtype} tensor on the GPU")
+def _ints(x: torch.Tensor, name: str, device: int, dtype=torch.int32) -> None:
+    if x.get_device() != device or x.dtype != dtype or not x.is_contiguous():
+        raise ValueError(f"{name} is a contiguous {dtype} tensor on the current GPU")
 
 
-# The current stream's handle without making a Stream object of it, which takes 3 us
-# of a call that takes 4.
-_raw_stream, _device = (getattr(torch._C, name, None) for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+# The current device and its stream's handle without making objects of them, which
+# takes 3 us of a call that takes 4.
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _handle(stream) -> int:
-    if stream is not None or _raw_stream is None or _device is None:
-        return _stream(stream)
-    return _raw_stream(_device())
+def _handle(stream, device: int) -> int:
+    return _stream(stream) if stream is not None or _raw_stream is None else _raw_stream(device)
+
+
+def _on(stream):
+    """Where a call's own tensors are made: memory used on a stream has to be that stream's."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
 
 def kv_plan(old: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: torch.Tensor, page_tokens: int, rows: int,
@@ -135,54 +140,64 @@ def kv_plan(old: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: tor
     from the front of ``free`` go into ``table`` [requests, max pages].  With
     ``check`` the call waits for the GPU and raises UzipError where a request
     took no part."""
-    _ints(old, "old")
-    _ints(new, "new")
-    _ints(free, "free")
-    _ints(table, "table")
+    device = _device()
+    _ints(old, "old", device)
+    _ints(new, "new", device)
+    _ints(free, "free", device)
+    _ints(table, "table", device)
     n = old.numel()
     if new.numel() != n or table.dim() != 2 or table.shape[0] != n:
         raise ValueError("old, new and table are of one batch")
     if out is None:
-        out = KVPlan(n, rows, page_tokens, old.device)
-    elif n > out.requests or not 0 <= rows <= out.rows or page_tokens < out.page_tokens:
-        raise ValueError("out is for fewer requests or rows, or larger pages")
+        with _on(stream):
+            out = KVPlan(n, rows, page_tokens, old.device)
+    elif n > out.requests or not 0 <= rows <= out.rows or page_tokens < out.page_tokens or out.lens.get_device() != device:
+        raise ValueError("out is for fewer requests or rows, larger pages or another GPU")
     rc = uzip_kv_plan(old.data_ptr(), new.data_ptr(), n, free.data_ptr(), free.numel(), page_tokens, rows, table.data_ptr(),
-                      table.shape[1], *out._ptrs, _handle(stream))
+                      table.shape[1], *out._ptrs, _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_kv_plan")
     if check:
-        (stream or torch.cuda.current_stream(old.device)).synchronize()
+        (stream or torch.cuda.current_stream()).synchronize()
         _check(int(out.status.item()), "uzip_kv_plan")
     return out
 
 
-def _rows(x: torch.Tensor, name: str, dim: int) -> int:
+def _rows(x: torch.Tensor, name: str, dim: int, device: int) -> int:
     t = _TYPES.get(x.dtype)
-    if t is None or not x.is_cuda or x.dim() != 3 or x.shape[2] != dim or (x.stride(2) != 1 and x.numel()):
+    if t is None or x.get_device() != device or x.dim() != 3 or x.shape[2] != dim or (x.stride(2) != 1 and x.numel()):
         raise ValueError(f"{name} is [rows, heads, {dim}] in bf16, fp16 or fp32 with each head's values side by side")
     return t
+
+
+def _current(cache: KVCache) -> int:
+    device = _device()
+    if cache.index != device:
+        raise ValueError("the cache is on another GPU than the current one")
+    return device
 
 
 def kv_store(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, runs: torch.Tensor,
              counts: torch.Tensor, stream=None) -> None:
     """Write rows of k and v [rows, heads, dim] to the places that kv_plan made."""
-    t = _rows(k, "k", cache.dim)
-    if _rows(v, "v", cache.dim) != t or k.shape != v.shape or k.shape[1] != cache.heads:
+    device = _current(cache)
+    t = _rows(k, "k", cache.dim, device)
+    if _rows(v, "v", cache.dim, device) != t or k.shape != v.shape or k.shape[1] != cache.heads:
         raise ValueError("k and v are [rows, the cache's heads, dim] of one type")
-    _ints(slots, "slots", torch.int64)
-    _ints(runs, "runs")
-    _ints(counts, "counts")
+    _ints(slots, "slots", device, torch.int64)
+    _ints(runs, "runs", device)
+    _ints(counts, "counts", device)
     rows = k.shape[0]
     if slots.numel() < rows or counts.numel() < 2 or runs.numel() != 2 * runs.shape[0]:
         raise ValueError("slots has an entry for each row, runs two for each run, counts two")
     rc = uzip_kv_store(cache, t, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), rows,
-                       slots.data_ptr(), runs.data_ptr(), counts.data_ptr(), runs.shape[0], _handle(stream))
+                       slots.data_ptr(), runs.data_ptr(), counts.data_ptr(), runs.shape[0], _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_kv_store")
 
 
 def kv_attend_workspace(q: torch.Tensor, cache: KVCache, requests: int, max_new: int) -> torch.Tensor:
-    t = _rows(q, "q", cache.dim)
+    t = _rows(q, "q", cache.dim, cache.index)
     n = uzip_kv_attend_workspace(t, q.shape[0], q.shape[1], cache.heads, cache.dim, requests, max_new)
     if n == 0:
         _check(EINVAL, "uzip_kv_attend_workspace")
@@ -194,30 +209,32 @@ def kv_attend(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: torch.
               lse: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None):
     """Causal attention of the new tokens q [rows, query heads, dim] over their
     requests' pages.  Returns (out like q, lse [rows, query heads] fp32)."""
-    t = _rows(q, "q", cache.dim)
+    device = _current(cache)
+    t = _rows(q, "q", cache.dim, device)
     rows, heads = q.shape[0], q.shape[1]
     n = lens.numel()
-    _ints(table, "table")
-    _ints(lens, "lens")
-    _ints(q_start, "q_start")
+    _ints(table, "table", device)
+    _ints(lens, "lens", device)
+    _ints(q_start, "q_start", device)
     if table.dim() != 2 or table.shape[0] < n or q_start.numel() <= n:
         raise ValueError("table, lens and q_start are of one batch")
     if not (0 <= window < 1 << 32 and 0 <= max_new < 1 << 32):
         raise ValueError("window and max_new are not negative")
-    if out is None:
-        out = torch.empty(rows, heads, cache.dim, dtype=q.dtype, device=q.device)
-    elif _rows(out, "out", cache.dim) != t or out.shape != q.shape:
+    if out is None or lse is None or ws is None:
+        with _on(stream):
+            out = torch.empty(rows, heads, cache.dim, dtype=q.dtype, device=q.device) if out is None else out
+            lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device) if lse is None else lse
+            ws = kv_attend_workspace(q, cache, n, max_new) if ws is None else ws
+    if _rows(out, "out", cache.dim, device) != t or out.shape != q.shape:
         raise ValueError("out is like q")
-    if lse is None:
-        lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device)
-    elif not (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]):
+    if lse.get_device() != device or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]:
         raise ValueError("lse is fp32 [rows, query heads]")
-    if ws is None:
-        ws = kv_attend_workspace(q, cache, n, max_new)
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise ValueError("ws is a contiguous tensor on the current GPU")
     rc = uzip_kv_attend(cache, t, q.data_ptr(), q.stride(0), q.stride(1), rows, heads, table.data_ptr(), table.shape[1],
                         lens.data_ptr(), q_start.data_ptr(), n, max_new, cache.dim ** -0.5 if scale is None else scale, window,
                         out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(), ws.data_ptr(),
-                        ws.numel() * ws.element_size(), _handle(stream))
+                        ws.numel() * ws.element_size(), _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_kv_attend")
     return out, lse

@@ -131,13 +131,14 @@ def test_store_refusals(uz):
 
 
 def test_plan_refusals(uz):
-    good = [64, 64, 2, 64, 8, 64, 10, 64, 4, 64, 64, 64, 64, 64, None, None]
+    good = [64, 64, 2, 64, 8, 64, 10, 64, 4, 128, 64, 64, 64, 64, None, None]
 
     def call(**at):
         a = list(good)
         for i, x in at.items():
             a[int(i[1:])] = x
         return uz.uzip_kv_plan(*a)
+    assert call(a9=64) == uz.EINVAL                                       # lengths out over lengths in
     for at, x in [(0, None), (0, 66), (1, None), (1, 66), (2, 4097), (3, None), (3, 66), (4, 1 << 31), (5, 24), (5, 0),
                   (6, (1 << 22) + 1), (7, None), (7, 66), (8, 1 << 31), (9, None), (9, 66), (10, None), (10, 66), (11, None),
                   (11, 68), (12, None), (12, 66), (13, None), (13, 66), (14, 66)]:
@@ -156,7 +157,7 @@ def test_attend_refusals(uz):
             a[int(i[1:])] = x
         return uz.uzip_kv_attend(*a)
     assert uz.uzip_kv_attend(None, *good[1:]) == uz.EINVAL
-    for at, x in [(1, 3), (1, -1), (2, None), (2, 65), (3, 1 << 40), (5, (1 << 22) + 1), (6, 0), (6, 3), (6, 1 << 20), (7, None),
+    for at, x in [(1, 3), (1, -1), (2, None), (2, 65), (3, 1 << 40), (5, (1 << 22) + 1), (5, 1 << 25), (6, 0), (6, 3), (6, 1 << 27), (7, None),
                   (7, 66), (8, 1 << 31), (9, None), (9, 66), (10, None), (10, 66), (11, 4097), (13, float("nan")),
                   (13, float("inf")), (15, None), (15, 65), (18, 66), (19, 72)]:
         assert call(**{f"a{at}": x}) == uz.EINVAL, (at, x)
