@@ -96,8 +96,9 @@ __device__ __forceinline__ bool sees(const Seen &s, int32_t t) { return (uint32_
 struct Lists {
   uint32_t least, most;
   uint32_t rows, shift;  // rows = 2^shift
-  uint32_t slots;  // first row of the workspace for their pieces
-  bool many;       // the many-rows kernel's
+  uint32_t slots;        // first row of the workspace for their pieces
+  bool many;             // the many-rows kernel's
+  uint32_t per_unit;     // then: pieces for a compute unit
 };
 
 struct Piece {
@@ -130,18 +131,22 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
 
 // How many steps make a piece, from the steps and blocks of all lists.
 //
-// Many rows: two pieces for each compute unit.
+// Many rows: two pieces for each compute unit, four of dim 64, whose workgroups are
+// lighter (512 new tokens of dim 64 over 14000: 145 us, by two 165).
 // Few rows: where there are fewer blocks than compute units, so that about one piece
-// comes to each (steps / S + blocks / 2 pieces come of S): one round of longer pieces
-// beats two of shorter ones, a piece's beginning and end being a few us (a request of
-// 100000 tokens, 8 heads: 49 us, with two to a unit 56; 8 requests of 2000 to 4000
-// tokens 22.5 and 29.6).  Where there are more, pieces of no less than 32 steps and up
-// to four to a unit, which even out requests of unlike lengths (64 requests of 1 to
-// 8000 tokens: 114 us, with one to a unit 130).
-constexpr uint32_t kFewPieces = 4, kManyPieces = 2, kLongPiece = 32;
-__device__ __forceinline__ uint32_t piece_steps(const AttendArgs &a, bool many, uint64_t steps, uint64_t blocks) {
-  const bool few_blocks = !many && blocks < a.units;
-  const uint32_t pieces = many ? kManyPieces * a.units : few_blocks ? a.units - (uint32_t)blocks / 2 : kFewPieces * a.units;
+// comes to each, and hardly ever a few more, which would be a second round (steps / S +
+// blocks / 2 pieces come of S, more where the blocks are alike): one round of longer
+// pieces beats two of shorter ones, a piece's beginning and end being a few us (a
+// request of 100000 tokens, 8 heads: 49 us, with two to a unit 56; 8 requests of 2000 to
+// 4000 tokens 22.5 and 29.6; 258 pieces where 192 do as well 42 and 32).  Where there
+// are more, pieces of no less than 32 steps and up to four to a unit, which even out
+// requests of unlike lengths (64 requests of 1 to 8000 tokens: 114 us, with one to a
+// unit 130).
+constexpr uint32_t kFewPieces = 4, kLongPiece = 32;
+constexpr uint32_t many_pieces(uint32_t dim) { return dim == 64 ? 4 : 2; }
+__device__ __forceinline__ uint32_t piece_steps(const AttendArgs &a, const Lists &l, uint64_t steps, uint64_t blocks) {
+  const bool many = l.many, few_blocks = !many && blocks < a.units;
+  const uint32_t pieces = many ? l.per_unit * a.units : few_blocks ? a.units - (uint32_t)blocks * 3 / 4 : kFewPieces * a.units;
   const uint32_t least = many || few_blocks ? kMinSteps : kLongPiece;
   if (steps <= (uint64_t)least * pieces) return least;
   return (uint32_t)min((steps + pieces - 1) / pieces, (uint64_t)INT32_MAX);
@@ -149,7 +154,7 @@ __device__ __forceinline__ uint32_t piece_steps(const AttendArgs &a, bool many, 
 
 // Which piece of the lists is number `index`, found by the whole workgroup.  A block
 // of n steps is split only where n > S = piece_steps, into ceil(n / S) < 2 n / S pieces:
-// with at most k units of pieces' worth of steps, k = kFewPieces or kManyPieces, there are at
+// with at most k units of pieces' worth of steps, k = kFewPieces or many_pieces, there are at
 // most k units + blocks pieces, k units split blocks and 2 k units slots of the
 // workspace.  With JOIN the index counts the blocks that were split instead.  Every
 // workgroup sums over the requests for itself: two scans.
@@ -189,7 +194,7 @@ __device__ bool find_piece(const AttendArgs &a, const Lists &lists, uint32_t ind
   }
   steps *= a.c.heads;
   blocks *= a.c.heads;
-  const uint32_t length = piece_steps(a, lists.many, steps, blocks);
+  const uint32_t length = piece_steps(a, lists, steps, blocks);
   auto count = [&](const Request &q, uint32_t *splits) {
     const uint32_t b = blocks_of(a, q, lists);
     const uint32_t n = steps_of(a, q, rows);
@@ -1156,7 +1161,7 @@ inline Layout layout(uzip_dtype type, uint32_t dim, uint32_t group, uint32_t max
   const uint64_t list = (uint64_t)max_new * group;
   const bool many = type != UZIP_FP32 && list > many_from(dim);
   const uint32_t few = many || list <= 16 ? 1 : 2;
-  return {many, few, 2 * (many ? kManyPieces * kManyBlock : 0) + 2 * kFewPieces * 16ull * few};
+  return {many, few, 2 * (many ? many_pieces(dim) * kManyBlock : 0) + 2 * kFewPieces * 16ull * few};
 }
 template <int D>
 uzip_status launch_attend(const AttendCall &call);

@@ -17,10 +17,10 @@ static uint32_t blocks_bound(const AttendArgs &a, const Lists &l) {
 }
 
 static uint32_t most_split(const AttendArgs &a, const Lists &l) {
-  return std::min(blocks_bound(a, l), (l.many ? kManyPieces : kFewPieces) * a.units);
+  return std::min(blocks_bound(a, l), (l.many ? l.per_unit : kFewPieces) * a.units);
 }
 static uint32_t most_pieces(const AttendArgs &a, const Lists &l) {
-  return blocks_bound(a, l) + (l.many ? kManyPieces : kFewPieces) * a.units;
+  return blocks_bound(a, l) + (l.many ? l.per_unit : kFewPieces) * a.units;
 }
 
 // No block has more than kMinSteps steps, so none is split.
@@ -40,11 +40,11 @@ template <int T, int CODE>
 static void launch(const AttendCall &c) {
   const AttendArgs &a = c.a;
   const Layout at = layout(c.type, KV_DIM, a.group, c.max_new);
-  const Lists few{1, at.many ? many_from(KV_DIM) : UINT32_MAX, 16 * at.few, at.few == 1 ? 4u : 5u, at.many ? 2 * kManyPieces * a.units * kManyBlock : 0, false};
+  const Lists few{1, at.many ? many_from(KV_DIM) : UINT32_MAX, 16 * at.few, at.few == 1 ? 4u : 5u, at.many ? 2 * many_pieces(KV_DIM) * a.units * kManyBlock : 0, false, 0};
   const uint32_t n_few = most_pieces(a, few);
   if constexpr (T != UZIP_FP32) {
     if (at.many) {
-      const Lists many{many_from(KV_DIM) + 1, UINT32_MAX, kManyBlock, 7, 0, true};
+      const Lists many{many_from(KV_DIM) + 1, UINT32_MAX, kManyBlock, 7, 0, true, many_pieces(KV_DIM)};
       const uint32_t n_many = most_pieces(a, many);
       all_rows_kernel<T, CODE, KV_DIM, 1><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
       join<T>(c, many, true, few);
