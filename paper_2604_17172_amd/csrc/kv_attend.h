@@ -47,12 +47,12 @@ constexpr int kMinSteps = 8;   // steps of a piece: two for each of a workgroup'
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
-// Lists of more rows than this go to the many-rows kernel, in blocks of 128 (32
-// requests of 1000 to 4000 tokens, 48 rows of dim 128: 100 us, by 16 x 3 or 64 rows at
-// a time 123; 36 rows of dim 256: 97 us, by 32 rows 66).  fp32 has none: its three terms
+// Lists of more rows than this go to the many-rows kernel, in blocks of 128, or of 64
+// where no list has more.  32 requests of 1000 to 4000 tokens, 48 rows of dim 128: in
+// blocks of 64 80 us, of 128 98, by the few-rows kernel 123; 36 rows of dim 256, 16
+// requests: by few rows 66 us, by many 97.  fp32 has no such kernel: its three terms
 // make the matrix units the bound, which few rows reach as well.
 constexpr uint32_t many_from(uint32_t dim) { return dim <= 128 ? 32 : 64; }
-constexpr uint32_t kManyBlock = 128;
 
 // ------------------------------------------------------------------ pieces of work
 struct Request {
@@ -423,14 +423,21 @@ __device__ __forceinline__ Frag class_frag(uint32_t lo, uint32_t hi, int kind) {
 __device__ __forceinline__ float class_value(int kind) { return kind == 0 ? NAN : kind == 1 ? INFINITY : -INFINITY; }
 
 // ------------------------------------------------------------------ few rows
-// One workgroup for up to 16 NM rows (NM 1 or 2) and a piece of their tokens, one wave a
-// step of 64 tokens, everything from memory straight into registers:
+// One workgroup for up to 16 NM rows (NM 1 or 2) and a piece of their tokens, one
+// wave a step of 64 tokens, everything from memory straight into registers:
 //   S^T = K Q^T, four tiles of 16 tokens: row m of tile i is token 16 (m / 4) + 4
 //   i + m % 4, so that a lane ends up with the scores of 16 tokens in a row for one
 //   query -- which is just what it needs of the second product's
 //   O^T = V^T P^T, whose first operand it loads as 16 bytes of a channel.
 // No score or code crosses lanes; pages of 16 tokens and more never split a lane's
 // load.  Each wave keeps its own maximum, sum and acc; they join at the end.
+//
+// Bound by the cache's bytes: the next step's keys are asked for when this one's
+// scores are done, its values after this one's products, so that 16 KiB (dim 128) of
+// each wave are under way.  4 requests of 120000 to 131072 tokens, 8 heads of 128: 1.03
+// GB in 180 us, 5.7 TB/s (a copy of 1 GiB: 5.1 read and written); 64 of up to 8191 and
+// 3 empty ones: 539 MB in 107 us, 5.0 TB/s.  The smallest call, 38 tokens: 6.7 us, of
+// which 3 are any launch's and the rest a chain of lengths, table, codes and joins.
 template <int D, int NM>
 struct FewRows {
   static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 16 * NM;
@@ -620,7 +627,7 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
           w.z = page_ok ? keep_tokens(w.z, t_lane + 8, lo, hi) : 0u;
           w.w = page_ok ? keep_tokens(w.w, t_lane + 12, lo, hi) : 0u;
         }
-        if (p_min != p_max || kLeaveOut<T, CODE>) {
+        if ((p_min != p_max && !all_see(t0)) || kLeaveOut<T, CODE>) {
           odd = odd || any_unbounded<CODE>(w);
           w = bounded<CODE>(w);
         }
@@ -757,9 +764,22 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
 // LDS holds codes, not bf16: half the bytes to read, for one conversion per two
 // codes and wave.  16-byte chunks are placed so that eight lanes next to each other
 // read eight different places of 128 bytes.
-template <int D>
+//
+// Bound by vector instructions: a wave's step has 32 matrix instructions and about 350
+// others (128 conversions; for each of 32 scores a multiply-add, an exponential, an
+// addition, half a maximum and half a rounding; the rest places and addresses).  Two
+// waves of a SIMD hide a matrix instruction behind about six others, and these take
+// 2 ns each.  A prompt of 8192 tokens, 32 heads over 8 of 128: 618 us, 890 TFLOP/s (a
+// bf16 matrix product of 8192: 1230); counters at that: matrix units 39% busy, vector
+// ALUs 63%.  Slower were: three waves to a SIMD (it spills), codes straight from memory
+// to registers (980 us then, with LDS 890), barriers every second step (the same), scores
+// of one tile during the softmax of another (740, 690 without).
+//
+// With PAIRS the block has 64 rows, two waves share 32 of them, and each takes one of
+// a step's two tiles of 32 tokens; their parts join at the end.
+template <int D, bool PAIRS>
 struct ManyRows {
-  static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves;
+  static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = PAIRS ? 64 : 128;
   static constexpr int kChunks = D / 16;              // of a key, and blocks of 16 channels
   static constexpr int kAll = kStep * kChunks, kLoads = (kAll + kThreads - 1) / kThreads;  // chunks of keys; of each thread; as many of values
   __device__ static __forceinline__ bool has(uint32_t n) { return kAll % kThreads == 0 || n < kAll; }
@@ -783,11 +803,11 @@ __device__ __forceinline__ f32x16 score_mfma32(const Frag &k, const Frag &q, f32
   else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.b, q.b, c, 0, 0, 0);
 }
 
-template <int T, int CODE, int D>
+template <int T, int CODE, int D, bool PAIRS>
 __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t index) {
-  typedef ManyRows<D> F;
+  typedef ManyRows<D, PAIRS> F;
   typedef typename Elem<T>::type Value;
-  constexpr int PROBS = Query<T>::kProbs, kTiles = kStep / 32, kChannels = D / 32, kKeySteps = D / 16;
+  constexpr int PROBS = Query<T>::kProbs, kTiles = PAIRS ? 1 : kStep / 32, kChannels = D / 32, kKeySteps = D / 16;
   __shared__ u32x4 keys[F::kRing][F::kAll];
   __shared__ u32x4 values[F::kRing][F::kAll];
   __shared__ float key_scale[F::kRing][4], value_scale[F::kRing][4];  // of 16 tokens each; a key's is -1 where there is no page
@@ -805,8 +825,8 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
   const uint32_t share = (steps + pc.splits - 1) / pc.splits;
   const uint32_t begin = step0 + min(steps, pc.split * share), end = step0 + min(steps, (pc.split + 1) * share);
 
-  // this wave's rows
-  const uint32_t w0 = r0 + 32 * wave, r = w0 + col;
+  // this wave's rows, and its first tile of a step's tokens
+  const uint32_t w0 = r0 + 32 * (PAIRS ? wave % 2 : wave), r = w0 + col, tile0 = PAIRS ? wave / 2 : 0;
   const bool here = r < list;
   const uint32_t tok = here ? r / a.group : 0, head = pc.head * a.group + (here ? r % a.group : 0);
   const Seen seen = seen_by(a, here ? pc.q.base + (int32_t)tok : -1);
@@ -883,10 +903,10 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
     }
     if (tid < 4) next_page = page_of(t0 + kStep + 16 * (int32_t)tid);
   };
-  auto put_one = [&](uint32_t b, int32_t t, bool edge, uint32_t n, const u32x4 &k, u32x4 w) {
+  auto put_one = [&](uint32_t b, int32_t t, bool edge, bool gaps, uint32_t n, const u32x4 &k, u32x4 w) {
     if (!F::has(n)) return;
     keys[b][F::key_at(n / F::kChunks, n % F::kChunks)] = k;
-    if (edge) {  // codes that no row sees count as zero, for 0 times NaN is not 0
+    if (edge || gaps) {  // codes that no row sees count as zero, for 0 times NaN is not 0
       w.x = stage_ok ? keep_tokens(w.x, t, lo, hi) : 0u;
       w.y = stage_ok ? keep_tokens(w.y, t + 4, lo, hi) : 0u;
       w.z = stage_ok ? keep_tokens(w.z, t + 8, lo, hi) : 0u;
@@ -901,8 +921,8 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
   auto put = [&](uint32_t step) {
     const uint32_t b = step % F::kRing;
     const int32_t t0 = (int32_t)(step * kStep), t = t0 + 16 * (int32_t)(tid % 4);
-    const bool edge = !all_see(t0) || !__all(stage_ok);
-    static_for<F::kLoads>([&](auto i) { put_one(b, t, edge, tid + F::kThreads * i, stage_k[i], stage_v[i]); });
+    const bool edge = !all_see(t0), gaps = !__all(stage_ok);
+    static_for<F::kLoads>([&](auto i) { put_one(b, t, edge, gaps, tid + F::kThreads * i, stage_k[i], stage_v[i]); });
     if (tid < 4) {
       key_scale[b][tid] = exp_ok ? pow2((int)stage_exp) : -1.0f;
       step_page[(step + 1) % F::kPages][tid] = next_page;
@@ -926,14 +946,14 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
     if (w0 < list && t0 <= p_max && (a.window == 0 || (int64_t)t0 + kStep - 1 > (int64_t)p_min - a.window)) {
       f32x16 s[kTiles];
       // The scores' products are issued before the other waves' softmax, which fills
-      // the gaps between them (with: 703 us, without: 717, a prompt of 8192).
+      // the gaps between them (with it 703 us, without 717, a prompt of 8192).
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
         s[i] = f32x16{};
 #pragma unroll
         for (int c = 0; c < kChannels; ++c) {
-          const u32x4 w = keys[b][F::key_at(32 * i + key_row, 2 * c + half)];
+          const u32x4 w = keys[b][F::key_at(32 * (tile0 + i) + key_row, 2 * c + half)];
           s[i] = score_mfma32<T>(key_frag<T, CODE>(w.x, w.y), q[2 * c], s[i]);
           s[i] = score_mfma32<T>(key_frag<T, CODE>(w.z, w.w), q[2 * c + 1], s[i]);
         }
@@ -943,11 +963,11 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
       bool page_ok[kTiles], pages_ok = true;
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-        const float x = key_scale[b][2 * i + half];
+        const float x = key_scale[b][2 * (tile0 + i) + half];
         page_ok[i] = x >= 0;
         pages_ok = pages_ok && page_ok[i];
         ks[i] = x * a.scale_log2;
-        vs[i] = value_scale[b][2 * i + half];
+        vs[i] = value_scale[b][2 * (tile0 + i) + half];
       }
       const bool whole = t0 + kStep - 1 <= p_min && (a.window == 0 || (int64_t)t0 > (int64_t)p_max - a.window) && __all(pages_ok);
       if (!whole) {
@@ -955,7 +975,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
         for (int i = 0; i < kTiles; ++i) {
 #pragma unroll
           for (int j = 0; j < 16; ++j)
-            s[i][j] = page_ok[i] && sees(seen, t0 + 32 * i + 16 * (int32_t)half + j) ? s[i][j] * ks[i] : -INFINITY;
+            s[i][j] = page_ok[i] && sees(seen, t0 + 32 * (int32_t)(tile0 + i) + 16 * (int32_t)half + j) ? s[i][j] * ks[i] : -INFINITY;
           ks[i] = 1;
         }
       }
@@ -994,7 +1014,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
       for (int i = 0; i < kTiles; ++i)
 #pragma unroll
         for (int c = 0; c < kChannels; ++c) {
-          const u32x4 w = values[b][F::value_at(32 * c + col, 2 * i + half)];
+          const u32x4 w = values[b][F::value_at(32 * c + col, 2 * (tile0 + i) + half)];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const Frag v = u ? codes_bf16<CODE>(w.z, w.w, vs[i]) : codes_bf16<CODE>(w.x, w.y, vs[i]);
@@ -1018,7 +1038,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
       for (int c = 0; c < kChannels; ++c)
 #pragma unroll 1
         for (int i = 0; i < kTiles; ++i) {
-          const int32_t t = t0 + 32 * i + 16 * (int32_t)half, page = page_of(t);
+          const int32_t t = t0 + 32 * (int32_t)(tile0 + i) + 16 * (int32_t)half, page = page_of(t);
           const bool ok = (uint32_t)page < a.c.n_pages;
           const u32x4 w = *(const u32x4 *)(a.c.v + ((size_t)(ok ? page : 0) * a.c.heads + pc.head) * page_bytes +
                                            (size_t)(32 * c + col) * P + ((uint32_t)t & (P - 1)));
@@ -1043,6 +1063,33 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
   }
 
   l += __shfl_xor(l, 32);
+  if constexpr (PAIRS) {  // the second wave's part over the codes' places, every wave being past them
+    __shared__ float pair_ml[2][64][2];
+    f32x4 *place = (f32x4 *)(wave == 2 || wave == 0 ? keys[0] : values[0]);
+    static_assert(sizeof(keys) >= kChannels * 4 * 64 * sizeof(f32x4), "a wave's acc");
+    if (tile0) {
+#pragma unroll
+      for (int c = 0; c < kChannels; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) place[(4 * c + i) * 64 + lane] = f32x4{acc[c][4 * i], acc[c][4 * i + 1], acc[c][4 * i + 2], acc[c][4 * i + 3]};
+      pair_ml[wave % 2][lane][0] = m;
+      pair_ml[wave % 2][lane][1] = l;
+    }
+    __syncthreads();
+    if (tile0) return;
+    const float m1 = pair_ml[wave][lane][0], m2 = fmaxf(m, m1);
+    const float s0 = m == m2 ? 1.0f : exp2_fast(m - m2), s1 = m1 == m2 ? 1.0f : exp2_fast(m1 - m2);
+    m = m2;
+    l = l * s0 + pair_ml[wave][lane][1] * s1;
+#pragma unroll
+    for (int c = 0; c < kChannels; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 x = place[(4 * c + i) * 64 + lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[c][4 * i + j] = acc[c][4 * i + j] * s0 + x[j] * s1;
+      }
+  }
   if (!here) return;
   const uint32_t in = r - r0;
   const int64_t row = pc.q.first + (int64_t)tok;
@@ -1073,7 +1120,9 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
 // ------------------------------------------------------------------ joining pieces
 // Pieces' maxima, sums and accs of the blocks that were split.  A wave takes a row
 // at a time: lanes in groups of dim / 4, four channels to a lane, each group every
-// so many pieces; `part` tells which 16 rows of the block.
+// so many pieces; `part` tells which 16 rows of the block.  Bound by latency: 6 us where
+// nothing was split, 7 for 32 blocks of 15 pieces, 14 for 144 blocks of 128 rows (a
+// wave's four rows at once took 22: where a block has few rows it loads them again).
 constexpr uint32_t kJoinRows = 16;
 template <int T, int D>
 __device__ void join_rows(const AttendArgs &a, const Lists &lists, bool last_first, uint32_t index, uint32_t part) {
@@ -1132,14 +1181,14 @@ __global__ __launch_bounds__(256, (kFewPerUnit<T, D, NM>)) void few_rows_kernel(
 }
 // Long lists and short ones in one launch: the first workgroups take the pieces of
 // the long ones, and the short ones' fill the gaps as they end.
-template <int T, int CODE, int D, int NM>
+template <int T, int CODE, int D, bool PAIRS>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void all_rows_kernel(AttendArgs a, Lists many, uint32_t n_many, Lists few) {
-  if (blockIdx.x < n_many) many_rows<T, CODE, D>(a, many, blockIdx.x);
-  else few_rows<T, CODE, D, NM>(a, few, blockIdx.x - n_many);
+  if (blockIdx.x < n_many) many_rows<T, CODE, D, PAIRS>(a, many, blockIdx.x);
+  else few_rows<T, CODE, D, 1>(a, few, blockIdx.x - n_many);
 }
 template <int T, int D>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, Lists many, uint32_t n_many, Lists few) {
-  const uint32_t of_many = kManyBlock / kJoinRows, of_few = few.rows / kJoinRows, i = blockIdx.x - n_many * of_many;
+  const uint32_t of_many = many.rows / kJoinRows, of_few = few.rows / kJoinRows, i = blockIdx.x - n_many * of_many;
   if (blockIdx.x < n_many * of_many) join_rows<T, D>(a, many, true, blockIdx.x / of_many, blockIdx.x % of_many);
   else join_rows<T, D>(a, few, false, i / of_few, i % of_few);
 }
@@ -1153,15 +1202,15 @@ struct AttendCall {
 };
 // What a call launches and where its pieces go.
 struct Layout {
-  bool many;              // the kernel for both, with blocks of 16 rows for the short lists
+  uint32_t many;          // 128 or 64: the kernel for both, with blocks of 16 rows for the short lists
   uint32_t few;           // blocks of 16 rows to a workgroup
   uint64_t rows_for_one;  // workspace rows for each compute unit
 };
 inline Layout layout(uzip_dtype type, uint32_t dim, uint32_t group, uint32_t max_new) {
   const uint64_t list = (uint64_t)max_new * group;
-  const bool many = type != UZIP_FP32 && list > many_from(dim);
+  const uint32_t many = type == UZIP_FP32 || list <= many_from(dim) ? 0 : list <= 64 ? 64 : 128;
   const uint32_t few = many || list <= 16 ? 1 : 2;
-  return {many, few, 2 * (many ? many_pieces(dim) * kManyBlock : 0) + 2 * kFewPieces * 16ull * few};
+  return {many, few, 2 * many_pieces(dim) * many + 2 * kFewPieces * 16ull * few};
 }
 template <int D>
 uzip_status launch_attend(const AttendCall &call);

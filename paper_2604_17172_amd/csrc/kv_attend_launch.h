@@ -32,7 +32,7 @@ template <int T>
 static void join(const AttendCall &c, const Lists &many, bool with_many, const Lists &few) {
   if (never_split(c.a)) return;
   const uint32_t n_many = with_many ? most_split(c.a, many) : 0, n_few = most_split(c.a, few);
-  const uint32_t grid = n_many * (kManyBlock / kJoinRows) + n_few * (few.rows / kJoinRows);
+  const uint32_t grid = n_many * (many.rows / kJoinRows) + n_few * (few.rows / kJoinRows);
   join_kernel<T, KV_DIM><<<grid, 256, 0, c.stream>>>(c.a, many, n_many, few);
 }
 
@@ -40,13 +40,16 @@ template <int T, int CODE>
 static void launch(const AttendCall &c) {
   const AttendArgs &a = c.a;
   const Layout at = layout(c.type, KV_DIM, a.group, c.max_new);
-  const Lists few{1, at.many ? many_from(KV_DIM) : UINT32_MAX, 16 * at.few, at.few == 1 ? 4u : 5u, at.many ? 2 * many_pieces(KV_DIM) * a.units * kManyBlock : 0, false, 0};
+  const Lists few{1, at.many ? many_from(KV_DIM) : UINT32_MAX, 16 * at.few, at.few == 1 ? 4u : 5u, 2 * many_pieces(KV_DIM) * a.units * at.many, false, 0};
   const uint32_t n_few = most_pieces(a, few);
   if constexpr (T != UZIP_FP32) {
     if (at.many) {
-      const Lists many{many_from(KV_DIM) + 1, UINT32_MAX, kManyBlock, 7, 0, true, many_pieces(KV_DIM)};
+      const Lists many{many_from(KV_DIM) + 1, UINT32_MAX, at.many, at.many == 64 ? 6u : 7u, 0, true, many_pieces(KV_DIM)};
       const uint32_t n_many = most_pieces(a, many);
-      all_rows_kernel<T, CODE, KV_DIM, 1><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
+      if constexpr (many_from(KV_DIM) < 64) {
+        if (at.many == 64) all_rows_kernel<T, CODE, KV_DIM, true><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
+      }
+      if (at.many == 128) all_rows_kernel<T, CODE, KV_DIM, false><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
       join<T>(c, many, true, few);
       return;
     }

