@@ -41,18 +41,22 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
+constexpr uint32_t kMostUnits = 256;  // compute units that the workspace is sized for, whatever the device
 constexpr int kStep = 64;      // tokens of a step
 constexpr int kMinSteps = 8;   // steps of a piece: two for each of a workgroup's waves
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
-// Lists of more rows than this go to the many-rows kernel, in blocks of 128, or of 64
-// where no list has more.  32 requests of 1000 to 4000 tokens, 48 rows of dim 128: in
-// blocks of 64 80 us, of 128 98, by the few-rows kernel 123; 36 rows of dim 256, 16
-// requests: by few rows 66 us, by many 97.  fp32 has no such kernel: its three terms
-// make the matrix units the bound, which few rows reach as well.
-constexpr uint32_t many_from(uint32_t dim) { return dim <= 128 ? 32 : 64; }
+// Lists of more rows than this go to the many-rows kernel, in blocks of 128.  By few
+// and by many rows, us, in bf16 (16 heads over 4):
+//   16 requests of 4000 tokens, 72 rows: dim 64 27 and 35, 96 29 and 48, 128 42 and 50,
+//   256 83 and 91; 32 of 96: 128 78 and 75, 256 164 and 154; 16 of 128: 64 35 and 36,
+//   96 39 and 50, 128 57 and 51; 8 of 128: 192 44 and 51, 256 71 and 59.
+// fp32 has no such kernel: its three terms make the matrix units the bound, which few
+// rows reach as well.
+constexpr uint32_t kManyRows = 128;
+constexpr uint32_t many_from(uint32_t dim) { return dim % 128 ? 128 : 96; }
 
 // ------------------------------------------------------------------ pieces of work
 struct Request {
@@ -774,12 +778,9 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
 // ALUs 63%.  Slower were: three waves to a SIMD (it spills), codes straight from memory
 // to registers (980 us then, with LDS 890), barriers every second step (the same), scores
 // of one tile during the softmax of another (740, 690 without).
-//
-// With PAIRS the block has 64 rows, two waves share 32 of them, and each takes one of
-// a step's two tiles of 32 tokens; their parts join at the end.
-template <int D, bool PAIRS>
+template <int D>
 struct ManyRows {
-  static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = PAIRS ? 64 : 128;
+  static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = kManyRows;
   static constexpr int kChunks = D / 16;              // of a key, and blocks of 16 channels
   static constexpr int kAll = kStep * kChunks, kLoads = (kAll + kThreads - 1) / kThreads;  // chunks of keys; of each thread; as many of values
   __device__ static __forceinline__ bool has(uint32_t n) { return kAll % kThreads == 0 || n < kAll; }
@@ -803,11 +804,11 @@ __device__ __forceinline__ f32x16 score_mfma32(const Frag &k, const Frag &q, f32
   else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.b, q.b, c, 0, 0, 0);
 }
 
-template <int T, int CODE, int D, bool PAIRS>
+template <int T, int CODE, int D>
 __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t index) {
-  typedef ManyRows<D, PAIRS> F;
+  typedef ManyRows<D> F;
   typedef typename Elem<T>::type Value;
-  constexpr int PROBS = Query<T>::kProbs, kTiles = PAIRS ? 1 : kStep / 32, kChannels = D / 32, kKeySteps = D / 16;
+  constexpr int PROBS = Query<T>::kProbs, kTiles = kStep / 32, kChannels = D / 32, kKeySteps = D / 16;
   __shared__ u32x4 keys[F::kRing][F::kAll];
   __shared__ u32x4 values[F::kRing][F::kAll];
   __shared__ float key_scale[F::kRing][4], value_scale[F::kRing][4];  // of 16 tokens each; a key's is -1 where there is no page
@@ -826,7 +827,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
   const uint32_t begin = step0 + min(steps, pc.split * share), end = step0 + min(steps, (pc.split + 1) * share);
 
   // this wave's rows, and its first tile of a step's tokens
-  const uint32_t w0 = r0 + 32 * (PAIRS ? wave % 2 : wave), r = w0 + col, tile0 = PAIRS ? wave / 2 : 0;
+  const uint32_t w0 = r0 + 32 * wave, r = w0 + col;
   const bool here = r < list;
   const uint32_t tok = here ? r / a.group : 0, head = pc.head * a.group + (here ? r % a.group : 0);
   const Seen seen = seen_by(a, here ? pc.q.base + (int32_t)tok : -1);
@@ -953,7 +954,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
         s[i] = f32x16{};
 #pragma unroll
         for (int c = 0; c < kChannels; ++c) {
-          const u32x4 w = keys[b][F::key_at(32 * (tile0 + i) + key_row, 2 * c + half)];
+          const u32x4 w = keys[b][F::key_at(32 * i + key_row, 2 * c + half)];
           s[i] = score_mfma32<T>(key_frag<T, CODE>(w.x, w.y), q[2 * c], s[i]);
           s[i] = score_mfma32<T>(key_frag<T, CODE>(w.z, w.w), q[2 * c + 1], s[i]);
         }
@@ -963,11 +964,11 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
       bool page_ok[kTiles], pages_ok = true;
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-        const float x = key_scale[b][2 * (tile0 + i) + half];
+        const float x = key_scale[b][2 * i + half];
         page_ok[i] = x >= 0;
         pages_ok = pages_ok && page_ok[i];
         ks[i] = x * a.scale_log2;
-        vs[i] = value_scale[b][2 * (tile0 + i) + half];
+        vs[i] = value_scale[b][2 * i + half];
       }
       const bool whole = t0 + kStep - 1 <= p_min && (a.window == 0 || (int64_t)t0 > (int64_t)p_max - a.window) && __all(pages_ok);
       if (!whole) {
@@ -975,7 +976,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
         for (int i = 0; i < kTiles; ++i) {
 #pragma unroll
           for (int j = 0; j < 16; ++j)
-            s[i][j] = page_ok[i] && sees(seen, t0 + 32 * (int32_t)(tile0 + i) + 16 * (int32_t)half + j) ? s[i][j] * ks[i] : -INFINITY;
+            s[i][j] = page_ok[i] && sees(seen, t0 + 32 * i + 16 * (int32_t)half + j) ? s[i][j] * ks[i] : -INFINITY;
           ks[i] = 1;
         }
       }
@@ -1014,7 +1015,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
       for (int i = 0; i < kTiles; ++i)
 #pragma unroll
         for (int c = 0; c < kChannels; ++c) {
-          const u32x4 w = values[b][F::value_at(32 * c + col, 2 * (tile0 + i) + half)];
+          const u32x4 w = values[b][F::value_at(32 * c + col, 2 * i + half)];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const Frag v = u ? codes_bf16<CODE>(w.z, w.w, vs[i]) : codes_bf16<CODE>(w.x, w.y, vs[i]);
@@ -1038,7 +1039,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
       for (int c = 0; c < kChannels; ++c)
 #pragma unroll 1
         for (int i = 0; i < kTiles; ++i) {
-          const int32_t t = t0 + 32 * (int32_t)(tile0 + i) + 16 * (int32_t)half, page = page_of(t);
+          const int32_t t = t0 + 32 * i + 16 * (int32_t)half, page = page_of(t);
           const bool ok = (uint32_t)page < a.c.n_pages;
           const u32x4 w = *(const u32x4 *)(a.c.v + ((size_t)(ok ? page : 0) * a.c.heads + pc.head) * page_bytes +
                                            (size_t)(32 * c + col) * P + ((uint32_t)t & (P - 1)));
@@ -1063,33 +1064,6 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
   }
 
   l += __shfl_xor(l, 32);
-  if constexpr (PAIRS) {  // the second wave's part over the codes' places, every wave being past them
-    __shared__ float pair_ml[2][64][2];
-    f32x4 *place = (f32x4 *)(wave == 2 || wave == 0 ? keys[0] : values[0]);
-    static_assert(sizeof(keys) >= kChannels * 4 * 64 * sizeof(f32x4), "a wave's acc");
-    if (tile0) {
-#pragma unroll
-      for (int c = 0; c < kChannels; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) place[(4 * c + i) * 64 + lane] = f32x4{acc[c][4 * i], acc[c][4 * i + 1], acc[c][4 * i + 2], acc[c][4 * i + 3]};
-      pair_ml[wave % 2][lane][0] = m;
-      pair_ml[wave % 2][lane][1] = l;
-    }
-    __syncthreads();
-    if (tile0) return;
-    const float m1 = pair_ml[wave][lane][0], m2 = fmaxf(m, m1);
-    const float s0 = m == m2 ? 1.0f : exp2_fast(m - m2), s1 = m1 == m2 ? 1.0f : exp2_fast(m1 - m2);
-    m = m2;
-    l = l * s0 + pair_ml[wave][lane][1] * s1;
-#pragma unroll
-    for (int c = 0; c < kChannels; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 x = place[(4 * c + i) * 64 + lane];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[c][4 * i + j] = acc[c][4 * i + j] * s0 + x[j] * s1;
-      }
-  }
   if (!here) return;
   const uint32_t in = r - r0;
   const int64_t row = pc.q.first + (int64_t)tok;
@@ -1170,20 +1144,28 @@ __device__ void join_rows(const AttendArgs &a, const Lists &lists, bool last_fir
 }
 
 // ------------------------------------------------------------------ kernels
+// Blocks of 32 rows read a list's tokens once where blocks of 16 read them twice, the
+// second time from a cache.  It pays where there are lists for every compute unit (64
+// requests of up to 8000 tokens, 4 heads with 32 rows: dim 64 in bf16 51 us, by blocks
+// of 16 59; 128 in bf16 95 and 109; 192 in bf16 135 and 147) and not where the
+// blocks of 16 are more work to share out (8 requests of 4000, 20 rows of dim 128: 33 and
+// 24).  Not at all in fp32, dim 256, or fp16 of dim 128, where registers spill (as above:
+// 136 and 125 in fp32, 148 and 112 in fp16; dim 256 in bf16 234 and 226).
+constexpr bool has_two(uint32_t type, uint32_t dim) { return type != UZIP_FP32 && dim <= 192 && !(type == UZIP_FP16 && dim == 128); }
 // Two workgroups to a compute unit where at most a few registers spill for it (32
-// requests, 20 rows of dim 128: 47 us, one to a unit 59; one row of dim 192: 50 and 55;
-// but of dim 256: 35 and 27).
+// requests, 20 rows of dim 128 in blocks of 32: 47 us, one to a unit 59; one row of dim
+// 192: 50 and 55; but of dim 256: 35 and 27).
 template <int T, int D, int NM>
-constexpr int kFewPerUnit = (D <= 128 ? T != UZIP_FP32 || NM == 1 : D == 192 && NM == 1 && T != UZIP_FP32) ? 2 : 1;
+constexpr int kFewPerUnit = (D <= 128 || (D == 192 && NM == 1 && T != UZIP_FP32)) ? 2 : 1;
 template <int T, int CODE, int D, int NM>
 __global__ __launch_bounds__(256, (kFewPerUnit<T, D, NM>)) void few_rows_kernel(AttendArgs a, Lists few) {
   few_rows<T, CODE, D, NM>(a, few, blockIdx.x);
 }
 // Long lists and short ones in one launch: the first workgroups take the pieces of
 // the long ones, and the short ones' fill the gaps as they end.
-template <int T, int CODE, int D, bool PAIRS>
+template <int T, int CODE, int D>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void all_rows_kernel(AttendArgs a, Lists many, uint32_t n_many, Lists few) {
-  if (blockIdx.x < n_many) many_rows<T, CODE, D, PAIRS>(a, many, blockIdx.x);
+  if (blockIdx.x < n_many) many_rows<T, CODE, D>(a, many, blockIdx.x);
   else few_rows<T, CODE, D, 1>(a, few, blockIdx.x - n_many);
 }
 template <int T, int D>
@@ -1202,15 +1184,16 @@ struct AttendCall {
 };
 // What a call launches and where its pieces go.
 struct Layout {
-  uint32_t many;          // 128 or 64: the kernel for both, with blocks of 16 rows for the short lists
+  bool many;              // the kernel for both, with blocks of 16 rows for the short lists
   uint32_t few;           // blocks of 16 rows to a workgroup
   uint64_t rows_for_one;  // workspace rows for each compute unit
 };
-inline Layout layout(uzip_dtype type, uint32_t dim, uint32_t group, uint32_t max_new) {
+inline Layout layout(uzip_dtype type, uint32_t dim, uint32_t heads, uint32_t group, uint32_t n_reqs, uint32_t max_new) {
   const uint64_t list = (uint64_t)max_new * group;
-  const uint32_t many = type == UZIP_FP32 || list <= many_from(dim) ? 0 : list <= 64 ? 64 : 128;
-  const uint32_t few = many || list <= 16 ? 1 : 2;
-  return {many, few, 2 * many_pieces(dim) * many + 2 * kFewPieces * 16ull * few};
+  const bool many = type != UZIP_FP32 && list > many_from(dim);
+  const bool two = !many && list > 16 && has_two(type, dim) && (uint64_t)n_reqs * heads >= kMostUnits;
+  const uint32_t few = two ? 2 : 1;
+  return {many, few, (many ? 2 * many_pieces(dim) * kManyRows : 0) + 2 * kFewPieces * 16ull * few};
 }
 template <int D>
 uzip_status launch_attend(const AttendCall &call);

@@ -8,8 +8,6 @@
 namespace uzip_kv {
 namespace {
 
-constexpr uint32_t kMostUnits = 256;  // compute units that the workspace is sized for, whatever the device
-
 bool attend_sizes(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_heads, uint32_t n_heads, uint32_t head_dim,
                   uint32_t n_reqs) {
   return valid_type(dtype) && valid_dim(head_dim) && n_heads > 0 && n_q_heads > 0 && n_q_heads % n_heads == 0 &&
@@ -27,7 +25,7 @@ extern "C" {
 size_t uzip_kv_attend_workspace(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_heads, uint32_t n_heads,
                                 uint32_t head_dim, uint32_t n_reqs, uint32_t max_new) {
   if (!attend_sizes(dtype, n_rows, n_q_heads, n_heads, head_dim, n_reqs)) return 0;
-  const Layout at = layout(dtype, head_dim, n_q_heads / n_heads, max_new);
+  const Layout at = layout(dtype, head_dim, n_heads, n_q_heads / n_heads, n_reqs, max_new);
   return (size_t)(kMostUnits * at.rows_for_one * (head_dim + 2) * sizeof(float));
 }
 
@@ -79,7 +77,7 @@ uzip_status uzip_kv_attend(const uzip_kv_cache *cache, uzip_dtype dtype, const v
   a.q_vec = at_multiples(d_q, q_row, q_head, 16);
   a.out_vec = at_multiples(d_out, out_row, out_head, 4 * bytes);
   a.part_acc = (float *)d_ws;
-  a.part_ml = a.part_acc + (size_t)kMostUnits * layout(dtype, cache->head_dim, a.group, max_new).rows_for_one * cache->head_dim;
+  a.part_ml = a.part_acc + (size_t)kMostUnits * layout(dtype, cache->head_dim, cache->n_heads, a.group, n_reqs, max_new).rows_for_one * cache->head_dim;
   call.type = dtype;
   call.code = cache->dtype;
   call.max_new = max_new;

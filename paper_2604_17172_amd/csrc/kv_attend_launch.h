@@ -39,23 +39,23 @@ static void join(const AttendCall &c, const Lists &many, bool with_many, const L
 template <int T, int CODE>
 static void launch(const AttendCall &c) {
   const AttendArgs &a = c.a;
-  const Layout at = layout(c.type, KV_DIM, a.group, c.max_new);
-  const Lists few{1, at.many ? many_from(KV_DIM) : UINT32_MAX, 16 * at.few, at.few == 1 ? 4u : 5u, 2 * many_pieces(KV_DIM) * a.units * at.many, false, 0};
+  const Layout at = layout(c.type, KV_DIM, a.c.heads, a.group, a.n_reqs, c.max_new);
+  const Lists few{1, at.many ? many_from(KV_DIM) : UINT32_MAX, 16 * at.few, at.few == 1 ? 4u : 5u,
+                  at.many ? 2 * many_pieces(KV_DIM) * a.units * kManyRows : 0, false, 0};
   const uint32_t n_few = most_pieces(a, few);
   if constexpr (T != UZIP_FP32) {
     if (at.many) {
-      const Lists many{many_from(KV_DIM) + 1, UINT32_MAX, at.many, at.many == 64 ? 6u : 7u, 0, true, many_pieces(KV_DIM)};
+      const Lists many{many_from(KV_DIM) + 1, UINT32_MAX, kManyRows, 7, 0, true, many_pieces(KV_DIM)};
       const uint32_t n_many = most_pieces(a, many);
-      if constexpr (many_from(KV_DIM) < 64) {
-        if (at.many == 64) all_rows_kernel<T, CODE, KV_DIM, true><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
-      }
-      if (at.many == 128) all_rows_kernel<T, CODE, KV_DIM, false><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
+      all_rows_kernel<T, CODE, KV_DIM><<<n_many + n_few, 256, 0, c.stream>>>(a, many, n_many, few);
       join<T>(c, many, true, few);
       return;
     }
   }
+  if constexpr (has_two(T, KV_DIM)) {
+    if (at.few == 2) few_rows_kernel<T, CODE, KV_DIM, 2><<<n_few, 256, 0, c.stream>>>(a, few);
+  }
   if (at.few == 1) few_rows_kernel<T, CODE, KV_DIM, 1><<<n_few, 256, 0, c.stream>>>(a, few);
-  else few_rows_kernel<T, CODE, KV_DIM, 2><<<n_few, 256, 0, c.stream>>>(a, few);
   join<T>(c, few, false, few);
 }
 

@@ -349,8 +349,58 @@ def test_attend_many_requests(uz):
 @pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("rows", [15, 17, 31, 33, 63, 65, 130])
 def test_attend_on_both_sides_of_the_kernels_lines(uz, dim, kind, rows):
-    """Lists of 16, 32 and 64 rows are where kernels change; a block has 16, 32 or 128."""
+    """Lists of 16 rows, and the ends of blocks of 16, 32 and 128."""
     attend_case(uz, 64, dim, 1, 1, kind, "e4m3fn", [700, 3], [rows, 1], fused=1)
+
+
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+def test_attend_where_the_kernel_for_many_rows_begins(uz, dim, kind):
+    """Lists of 96 or 128 rows, by dim, and the next."""
+    for rows in (95, 96, 97, 127, 128, 129):
+        attend_case(uz, 64, dim, 1, 1, kind, "e4m3fn", [300, 3], [rows, 2], seed=22)
+    attend_case(uz, 16, dim, 2, 5, kind, "e5m2", [700, 0, 40, 5], [20, 30, 26, 19], seed=23, window=333)
+
+
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
+def test_attend_lists_of_17_to_32_rows_for_every_unit(uz, dim, kind):
+    """Requests times heads past the compute units: blocks of 32 rows where there are such; one long list is split."""
+    g = np.random.default_rng(24)
+    ctx, new = g.integers(0, 90, 90), g.integers(0, 9, 90)
+    ctx[7], new[7], new[8] = 3000, 8, 8
+    attend_case(uz, 32, dim, 3, 4, kind, "e4m3fn", ctx.tolist(), new.tolist(), seed=25)
+    attend_case(uz, 16, dim, 3, 6, kind, "e5m2", ctx.tolist(), np.minimum(new, 5).tolist(), seed=26, window=50, holes=True)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+def test_attend_nan_and_infinity_in_blocks_of_32_rows(uz, fmt, kind):
+    g = np.random.default_rng(74)
+    n, total, new, page, dim = 130, 40, 9, 16, 64
+    side = Side(uz, 3 * n, 2, page, dim, fmt, g)
+
+    def edit(x, d):
+        for t in (x, d):
+            if edit.values:
+                for i in range(0, n, 3):
+                    for tok, ch, v in ((33, 3, "nan"), (35, 3, "inf"), (36, 5, "-inf"), (38, 6, "inf"), (39, 6, "-inf"), (2, 9, "inf")):
+                        t[i * total + tok, i % 2, ch] = float(v)
+        edit.values = True
+    edit.values = False
+    _, want, _ = grow(uz, side, [0] * n, [total] * n, np.full((n, 4), -1, np.int32), np.arange(3 * n, dtype=np.int32), kind, g, edit=edit)
+    q, qd = rows_of((n * new, 4, dim), kind, g)
+    q_start = np.arange(n + 1, dtype=np.int32) * new
+    for window in (0, 12):
+        with np.errstate(invalid="ignore"):
+            expect = ref.attend(np_of(q), side.k, side.k_exp, side.v, side.v_exp, fmt, want["table"], [total] * n, q_start, page, 0.1, window)
+        out, lse = run_attend(uz, side, qd, ints(want["table"]), ints([total] * n), ints(q_start), new, 0.1, window)
+        got, fine = np_of(out), np.isfinite(expect["out"])
+        assert not fine.all() and fine.any()
+        assert np.array_equal(got[~fine], expect["out"][~fine], equal_nan=True)
+        assert np.isfinite(got[fine]).all()
+        clean = {k: np.where(fine, v, 0.0) if k in ("out", "spread") else v for k, v in expect.items()}
+        check_attend((torch.from_numpy(np.where(fine, got, 0.0)), lse), clean, kind, dim, total)
 
 
 @pytest.mark.parametrize("kind,dim,ctx", [("bf16", 128, 5000), ("fp16", 64, 4097), ("fp32", 96, 3333)])
@@ -460,7 +510,7 @@ def test_attend_nan_and_infinity_reach_only_rows_that_see_them(uz, fmt, kind, ne
 
 @pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
-@pytest.mark.parametrize("new", [3, 20, 50])
+@pytest.mark.parametrize("new", [3, 20, 50, 80])
 def test_attend_nan_beside_a_page_that_is_none(uz, fmt, kind, new):
     """A NaN that all rows see, in a step of which another page is missing, reaches all rows."""
     g = np.random.default_rng(73)
