@@ -51,12 +51,13 @@ __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_lo
 // Lists of more rows than this go to the many-rows kernel, in blocks of 128.  By few
 // and by many rows, us, in bf16 (16 heads over 4):
 //   16 requests of 4000 tokens, 72 rows: dim 64 27 and 35, 96 29 and 48, 128 42 and 50,
-//   256 83 and 91; 32 of 96: 128 78 and 75, 256 164 and 154; 16 of 128: 64 35 and 36,
-//   96 39 and 50, 128 57 and 51; 8 of 128: 192 44 and 51, 256 71 and 59.
+//   256 83 and 91; 32 of 96 rows: 128 78 and 75, 256 164 and 154; 16 of 160 rows: 64 38
+//   and 42, 96 44 and 64, 192 72 and 116; 16 of 256: 64 49 and 43, 96 56 and 67, 192 101
+//   and 122; but 4 of 60000 tokens, 200 rows: 96 232 and 188, 192 339 and 330.
 // fp32 has no such kernel: its three terms make the matrix units the bound, which few
 // rows reach as well.
 constexpr uint32_t kManyRows = 128;
-constexpr uint32_t many_from(uint32_t dim) { return dim % 128 ? 128 : 96; }
+constexpr uint32_t many_from(uint32_t dim) { return dim % 128 ? 160 : 96; }
 
 // ------------------------------------------------------------------ pieces of work
 struct Request {
@@ -143,13 +144,16 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
 // pieces beats two of shorter ones, a piece's beginning and end being a few us (a
 // request of 100000 tokens, 8 heads: 49 us, with two to a unit 56; 8 requests of 2000 to
 // 4000 tokens 22.5 and 29.6; 258 pieces where 192 do as well 42 and 32).  Where there
-// are more, pieces of no less than 32 steps and up to four to a unit, which even out
-// requests of unlike lengths (64 requests of 1 to 8000 tokens: 114 us, with one to a
-// unit 130).
+// are more, or at least half as many as units and long ones (18 requests of 7500 to
+// 30000 tokens, 8 heads of 128, 144 blocks: 147 us, by the rule above 160; of dim 64 76
+// and 111; 20 of 1000 to 4000 of dim 256 by that rule 54, by this one 66), pieces of no
+// less than 32 steps and up to four to a unit, which even out requests of unlike
+// lengths (64 requests of 1 to 8000 tokens: 114 us, with one to a unit 130).
 constexpr uint32_t kFewPieces = 4, kLongPiece = 32;
 constexpr uint32_t many_pieces(uint32_t dim) { return dim == 64 ? 4 : 2; }
 __device__ __forceinline__ uint32_t piece_steps(const AttendArgs &a, const Lists &l, uint64_t steps, uint64_t blocks) {
-  const bool many = l.many, few_blocks = !many && blocks < a.units;
+  const bool many = l.many;
+  const bool few_blocks = !many && blocks < a.units && (2 * blocks < a.units || steps < 2 * kLongPiece * blocks);
   const uint32_t pieces = many ? l.per_unit * a.units : few_blocks ? a.units - (uint32_t)blocks * 3 / 4 : kFewPieces * a.units;
   const uint32_t least = many || few_blocks ? kMinSteps : kLongPiece;
   if (steps <= (uint64_t)least * pieces) return least;

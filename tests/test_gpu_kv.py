@@ -356,8 +356,8 @@ def test_attend_on_both_sides_of_the_kernels_lines(uz, dim, kind, rows):
 @pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
 def test_attend_where_the_kernel_for_many_rows_begins(uz, dim, kind):
-    """Lists of 96 or 128 rows, by dim, and the next."""
-    for rows in (95, 96, 97, 127, 128, 129):
+    """Lists of 96 or 160 rows, by dim, and the next; blocks of 128 and what is left of them."""
+    for rows in (95, 96, 97, 127, 128, 129, 160, 161, 256, 257):
         attend_case(uz, 64, dim, 1, 1, kind, "e4m3fn", [300, 3], [rows, 2], seed=22)
     attend_case(uz, 16, dim, 2, 5, kind, "e5m2", [700, 0, 40, 5], [20, 30, 26, 19], seed=23, window=333)
 
@@ -371,6 +371,13 @@ def test_attend_lists_of_17_to_32_rows_for_every_unit(uz, dim, kind):
     ctx[7], new[7], new[8] = 3000, 8, 8
     attend_case(uz, 32, dim, 3, 4, kind, "e4m3fn", ctx.tolist(), new.tolist(), seed=25)
     attend_case(uz, 16, dim, 3, 6, kind, "e5m2", ctx.tolist(), np.minimum(new, 5).tolist(), seed=26, window=50, holes=True)
+
+
+@pytest.mark.parametrize("dim,kind", [(64, "bf16"), (128, "fp16"), (256, "fp32")])
+def test_attend_long_lists_for_half_the_units(uz, dim, kind):
+    """136 blocks of long requests, and of less long ones: where the length of a piece changes its rule."""
+    attend_case(uz, 128, dim, 8, 1, kind, "e4m3fn", [4200] * 17, [1] * 17, seed=27)
+    attend_case(uz, 128, dim, 8, 1, kind, "e4m3fn", [4200] * 16 + [3], [2] * 17, seed=28, window=3000)
 
 
 @pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
@@ -510,7 +517,7 @@ def test_attend_nan_and_infinity_reach_only_rows_that_see_them(uz, fmt, kind, ne
 
 @pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
-@pytest.mark.parametrize("new", [3, 20, 50, 80])
+@pytest.mark.parametrize("new", [3, 20, 50, 90])
 def test_attend_nan_beside_a_page_that_is_none(uz, fmt, kind, new):
     """A NaN that all rows see, in a step of which another page is missing, reaches all rows."""
     g = np.random.default_rng(73)
