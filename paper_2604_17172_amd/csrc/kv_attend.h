@@ -777,7 +777,7 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
 // others (128 conversions; for each of 32 scores a multiply-add, an exponential, an
 // addition, half a maximum and half a rounding; the rest places and addresses).  Two
 // waves of a SIMD hide a matrix instruction behind about six others, and these take
-// 2 ns each.  A prompt of 8192 tokens, 32 heads over 8 of 128: 618 us, 890 TFLOP/s (a
+// 2 ns each.  A prompt of 8192 tokens, 32 heads over 8 of 128: 625 us, 880 TFLOP/s (a
 // bf16 matrix product of 8192: 1230); counters at that: matrix units 39% busy, vector
 // ALUs 63%.  Slower were: three waves to a SIMD (it spills), codes straight from memory
 // to registers (980 us then, with LDS 890), barriers every second step (the same), scores
