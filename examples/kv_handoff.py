@@ -40,14 +40,19 @@ class Instance:
 
     def taken(self, plan) -> None:
         """The lengths and the free list after a step."""
-        if int(plan.status.item()) != uz.OK:
-            raise uz.UzipError(int(plan.status.item()), "uzip_kv_plan")
+        granted(plan)
         self.lens.copy_(plan.lens)
         self.free = self.free[int(plan.counts[0]):].contiguous()
 
     def give(self, pages: int) -> torch.Tensor:
         mine, self.free = self.free[:pages].clone(), self.free[pages:].contiguous()
         return mine
+
+
+def granted(plan) -> None:
+    """Every request of the step had its places."""
+    if int(plan.status.item()) != uz.OK:
+        raise uz.UzipError(int(plan.status.item()), "uzip_kv_plan")
 
 
 def send(side: Instance, pages: torch.Tensor):
@@ -119,6 +124,7 @@ def main(prompts=(1000, 37, 2050), answer: int = 70) -> float:
         qkv.copy_(tokens(n))
         free.copy_(writer_free[:n])
         graph.replay()
+        granted(step_plan)
         writer.lens.copy_(step_plan.lens)
         writer_free = writer_free[int(step_plan.counts[0]):].contiguous()
         stayed, want, _ = reader.step(qkv, one, 1)                   # the same tokens over the cache that stayed

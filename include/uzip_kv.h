@@ -83,8 +83,8 @@ uint32_t uzip_kv_max_runs(uint32_t n_rows, uint32_t n_reqs, uint32_t page_tokens
  *                request that go to one page; entries past the count are
  *                not written
  *   d_counts:    [2]          pages taken from d_free; runs
- *   d_status:    device u32 (may be NULL), written on an error only: the caller
- *                zeroes it.
+ *   d_status:    device u32 (may be NULL): this call's UZIP_OK or error, whatever
+ *                it held before, so each replay of a graph gives its own
  * A request whose pages are not to be had -- d_free at its end, or more than
  * max_pages of them (UZIP_ENOSPC) -- or whose lengths are negative or whose
  * rows do not fit n_rows (UZIP_EINVAL) takes no part: d_lens reads 0, its slots

@@ -88,7 +88,7 @@ __device__ Sums block_scan(const Sums &v, const Sums &limit, Sums *part, Sums *t
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   extern __shared__ int32_t lds[];
   __shared__ Sums part[kPlanThreads / 64];
-  __shared__ int trouble;
+  __shared__ int trouble, worst;
   const uint32_t tid = threadIdx.x, n = a.n_reqs, P = 1u << a.shift;
   int32_t *first_row = lds, *first_page = lds + n + 1, *first_run = first_page + n;  // first_page -1: takes no part
   const Sums limit = {a.n_rows + 1, a.n_free + 1, a.n_rows + 1};
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   };
   auto clamp_pages = [&](int64_t x) { return (uint32_t)min(max(x, (int64_t)0), (int64_t)limit.pages); };
 
-  if (tid == 0) trouble = 0;
+  if (tid == 0) trouble = worst = 0;
   __syncthreads();
   Sums done = {0, 0, 0};
   int error = 0;
@@ -191,9 +191,10 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
       a.counts[0] = (int32_t)done.pages;
       a.counts[1] = (int32_t)done.runs;
     }
-    if (error && a.status) atomicMin(a.status, error);
+    if (error) atomicMin(&worst, error);
   }
   __syncthreads();
+  if (blockIdx.x == 0 && tid == 0 && a.status) *a.status = worst;
 
   for (uint32_t i = blockIdx.x * kPlanThreads + tid; i <= n; i += gridDim.x * kPlanThreads) {
     a.q_start[i] = first_row[i];

@@ -92,7 +92,7 @@ class KVCache:
 class KVPlan:
     """A step's places, on the GPU (see uzip_kv_plan), for up to ``requests`` requests and ``rows`` new tokens: lens
     int32 [requests], q_start int32 [requests + 1], slots int64 [rows], runs int32 [max runs, 2], counts int32 [2]
-    (pages taken, runs), status int32 [1]."""
+    (pages taken, runs), status int32 [1] (of the last call)."""
 
     __slots__ = ("requests", "rows", "page_tokens", "lens", "q_start", "slots", "runs", "counts", "status", "_ptrs")
 
