@@ -48,6 +48,13 @@ constexpr int kMinSteps = 8;   // steps of a piece: two for each of a workgroup'
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
+// How far a score may pass the running maximum before that is taken anew: weights up
+// to 2^8 cost no precision, and most steps need no exchange between lanes and no
+// rescaling.  Such weights must not push the sum of weights times values out of range:
+// 2^8, 2^31 tokens, codes below 2^16 and scales up to 2^72 stay below 2^127.  A step with a
+// larger scale lets no score pass, so that each of its weights is at most 1.
+__device__ __forceinline__ float lag_for(float value_scale) { return value_scale > 0x1p72f ? 0.0f : 8.0f; }
+
 // Lists of more rows than this go to the many-rows kernel, in blocks of 128.  By few
 // and by many rows, us, in bf16 (16 heads over 4):
 //   16 requests of 4000 tokens, 72 rows: dim 64 27 and 35, 96 29 and 48, 128 42 and 50,
@@ -586,9 +593,7 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
       c = 1;
     }
 
-    // The maximum is taken anew only where a score passes the old one by more
-    // than 8: powers of two up to 2^8 cost no precision, and most steps need
-    // no exchange between lanes and no rescaling.
+    const float lag = lag_for(vs);
     Frag p[NM][2][PROBS];
 #pragma unroll
     for (int n = 0; n < NM; ++n) {
@@ -598,7 +603,7 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
 #pragma unroll
         for (int j = 0; j < 4; ++j) top = fmaxf(top, s[n][i][j]);
       top *= c;
-      if (__any(top > m[n] + 8.0f)) {
+      if (__any(top > m[n] + lag)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float m2 = fmaxf(m[n], top);
@@ -964,6 +969,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
         }
       }
       __builtin_amdgcn_s_setprio(0);
+      static_assert(kTiles == 2, "two scales to a lane's part of a step");
       float ks[kTiles], vs[kTiles];  // ks: what a score is still to be multiplied by
       bool page_ok[kTiles], pages_ok = true;
 #pragma unroll
@@ -992,7 +998,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
         for (int j = 1; j < 16; ++j) t = fmaxf(t, s[i][j]);
         top = fmaxf(top, t * ks[i]);
       }
-      if (__any(top > m + 8.0f)) {
+      if (__any(top > m + lag_for(fmaxf(vs[0], vs[1])))) {
         top = fmaxf(top, __shfl_xor(top, 32));
         const float m2 = fmaxf(m, top);
         const float shrink = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);

@@ -3,7 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_kv import ints, uz  # noqa: F401
+from oracle import kv as ref
+from test_gpu_kv import Side, check_attend, dev, ints, np_of, rows_of, run_attend, say, uz  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,57 @@ def test_each_replay_of_a_plan_has_its_own_status(uz):
         graph.replay()
         torch.cuda.synchronize()
         assert int(plan.status.item()) == status, tokens
+
+
+# ------------------------------------------------------------------ attention: chosen scores and values
+class Scored(Side):
+    """One request of `total` tokens, one head: token t scores scores[t] (else 0) for a query that is 1 in channel 0."""
+
+    def __init__(self, uz, fmt, total, dim, scores, page=16, seed=91):
+        g = np.random.default_rng(seed)
+        pages = -(-total // page)
+        super().__init__(uz, pages, 1, page, dim, fmt, g)
+        self.total, self.table = total, g.permutation(pages).astype(np.int32)[None]
+        self.k[:], self.k_exp[:], self.v_exp[:] = 0, 127, 127
+        self.v[:] = ref.encode(g.standard_normal(self.v.shape), fmt)
+        for t, s in scores.items():
+            self.k[self.at(t)][0] = ref.encode(s, fmt)
+        self.g = g
+
+    def at(self, t):
+        return self.table[0, t // self.page], 0, t % self.page
+
+    def value(self, t, ch, x):
+        self.v[self.at(t)][ch] = ref.encode(x, self.fmt)
+
+    def attend(self, uz, kind, new, window=0, group=1):
+        for mine, its in ((self.k, self.cache.k), (self.v.transpose(0, 1, 3, 2), self.cache.v), (self.k_exp, self.cache.k_exp),
+                          (self.v_exp, self.cache.v_exp)):
+            its.copy_(dev(mine))
+        q, qd = rows_of((new, group, self.dim), kind, self.g)
+        q[:, :, 0] = 1
+        qd[:, :, 0] = 1
+        with np.errstate(invalid="ignore"):
+            want = ref.attend(np_of(q), self.k, self.k_exp, self.v, self.v_exp, self.fmt, self.table, [self.total], [0, new],
+                              self.page, 1.0, window)
+        return want, run_attend(uz, self, qd, ints(self.table), ints([self.total]), ints([0, new]), new, 1.0, window)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("total,new", [(300, 1), (321, 1), (330, 10), (530, 200), (5000, 2)])
+def test_attend_values_near_the_end_of_32_bits(uz, fmt, kind, total, new):
+    """A token that scores 5 (a factor of 2^7.2) more than those before it, with values of 2^127: sums whose single weights are
+    at most 1 stay finite, whichever step the token comes in."""
+    say("large values", fmt, kind, total, new)
+    top, last = ref.FORMATS[fmt][2], ref.FORMATS[fmt][3]
+    for hot, score in ((5, 0.0), (70, 5.0), (261, 5.0), (total - new, 5.0)):
+        side = Scored(uz, fmt, total, 64, {hot: score})
+        pg = side.at(hot)[0]
+        side.v[pg] = 0
+        side.v_exp[pg] = last
+        for ch in range(0, 64, 3):
+            side.value(hot, ch, -top if ch % 2 else top)
+        want, got = side.attend(uz, kind, new)
+        assert np.isfinite(want["out"]).all() and np.abs(want["out"]).max() > 1e34
+        check_attend(got, want, kind, 64, total)
