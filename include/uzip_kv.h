@@ -131,9 +131,10 @@ size_t uzip_kv_attend_workspace(uzip_dtype dtype, uint32_t n_rows, uint32_t n_q_
  * d_q_start[n_reqs]) gives zeros and -infinity.  Products and sums are held in
  * 32 bits; probabilities enter the second product with at least 8 bits for
  * bf16, 16 for fp16 and 24 for fp32.
- * Scores are scale * 2^(k_exp - 127) times the products of queries with codes, and out
- * is a sum of weights of at most 1 times values, over the sum of the weights: where one
- * of these passes the largest 32-bit number the results are not finite.
+ * A value that is infinite or NaN is so for every row that sees it, however small its
+ * weight.  Scores are scale * 2^(k_exp - 127) times the products of queries with codes,
+ * and out is a sum of weights of at most 1 times values, over the sum of the weights:
+ * where one of these passes the largest 32-bit number the results are not finite.
  *   max_new:     the most new tokens of a request.  It chooses kernels: a wrong
  *                value costs time, and the last bits may differ.
  *   d_table, max_pages, d_lens, d_q_start, n_reqs: as uzip_kv_plan leaves them; a

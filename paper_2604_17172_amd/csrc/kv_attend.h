@@ -249,7 +249,18 @@ __device__ bool find_piece(const AttendArgs &a, const Lists &lists, uint32_t ind
     at += c;
   }
   __syncthreads();
-  *out = found;
+  if (JOIN) {
+    *out = found;
+    return true;
+  }
+  // The same in all lanes, which the compiler is to know: it then holds them once for a
+  // wave, and few spill where the kernel holds a second computation of its piece (64
+  // requests, dim 128 in blocks of 32: 73 us, else 97).
+  uint32_t words[sizeof(Piece) / 4];
+  __builtin_memcpy(words, &found, sizeof(Piece));
+#pragma unroll
+  for (uint32_t i = 0; i < sizeof(Piece) / 4; ++i) words[i] = __builtin_amdgcn_readfirstlane(words[i]);
+  __builtin_memcpy(out, words, sizeof(Piece));
   return true;
 }
 
@@ -281,11 +292,25 @@ struct Query<UZIP_FP32> {  // 24 bits: three bf16 terms each
   static constexpr int kTerms = 3, kProbs = 3;
 };
 
-// Infinities (e5m2 has them) times the second and third term of a probability,
-// which may be 0 or negative, are no infinities: there they are always left out of
-// the product and added after it.
-template <int T, int CODE>
-constexpr bool kLeaveOut = CODE == UZIP_E5M2 && Query<T>::kProbs > 1;
+// An infinite value or a NaN is what it is for every row that sees it, however small
+// its weight, and nothing for a row that does not.  Products do not give that: a weight
+// of 0, or a later term of a probability, which may be 0 or negative, times it is no
+// infinity, and a factor of 0 on a sum that holds it neither.  A piece is computed as if
+// there were none; if its sums come out not finite, it is computed again with such
+// codes left out, and they are added after that.  A test of every step's codes instead
+// costs up to half (e5m2, dim 128 in blocks of 32: 111 us, this 73; dim 192 61 and 47).
+__device__ __forceinline__ float not_finite(float so_far, f32x4 x) {  // NaN from the first infinity or NaN on, else 0
+#pragma unroll
+  for (int j = 0; j < 4; ++j) so_far = __builtin_fmaf(x[j], 0.0f, so_far);
+  return so_far;
+}
+
+// x * w, w >= 0, where an infinity stays one whatever w is.
+__device__ __forceinline__ f32x4 weighed(f32x4 x, float w) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = fabsf(x[j]) == INFINITY ? x[j] : x[j] * w;
+  return x;
+}
 
 union Frag {
   bf16x8 b;
@@ -459,16 +484,23 @@ struct FewRows {
   static constexpr int kPairs = D / 64, kOdd = (D / 32) % 2, kKeySteps = D / 32, kChannels = D / 16;
 };
 
-template <int T, int CODE, int D, int NM>
-__device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index) {
+// Without LEAVE_OUT false where a NaN or an infinity was met: then nothing was written,
+// and the piece is computed from its beginning with it, so that nothing is kept in
+// registers for that (a loop around the steps alone: dim 256 102 us, this 78).
+template <int T, int CODE, int D, int NM, bool LEAVE_OUT>
+__device__ __forceinline__ bool few_rows_piece(const AttendArgs &a, const Lists &lists, uint32_t index,
+                                               float (&join_acc)[2][16 * NM][D + 4],
+                                               float (&join_ml)[FewRows<D, NM>::kWaves][16 * NM][2],
+                                               uint32_t (&join_odd)[FewRows<D, NM>::kWaves]) {
   typedef FewRows<D, NM> F;
   typedef typename Elem<T>::type Value;
   constexpr int TERMS = Query<T>::kTerms, PROBS = Query<T>::kProbs;
-  __shared__ float join_acc[2][F::kRows][D + 4];
-  __shared__ float join_ml[F::kWaves][F::kRows][2];
   Piece pc;
-  if (!find_piece<F::kThreads, false>(a, lists, index, &pc)) return;
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+  if (!find_piece<F::kThreads, false>(a, lists, index, &pc)) return true;
+  const uint32_t lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  // one number for a wave in blocks of 32, whose registers are short (dim 128: 73 us, else
+  // 82), but not in blocks of 16 (64 requests, dim 128: 106 us, without 104)
+  const uint32_t wave = NM == 2 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x >> 6;
   const uint32_t list = (uint32_t)pc.q.rows * a.group, r0 = pc.block * F::kRows, P = a.c.page;
   int32_t lo, hi;
   seen_range(a, pc.q, r0, min(list, r0 + F::kRows), &lo, &hi);
@@ -541,7 +573,6 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
 
   uint32_t step = begin + wave;
   int32_t key_page = -1, value_page = -1;
-  bool odd = false;  // a NaN or an infinity was left out
   if (step < end) {
     const int32_t t0 = (int32_t)(step * kStep);
     key_page = page_of(t0 + key_chunk);
@@ -628,24 +659,21 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
         }
     }
 
-    // Codes that no row sees count as zero, for 0 times NaN is not 0.  A NaN or an
-    // infinity that some rows see and others do not is left for after the loop.
-    if (!whole || kLeaveOut<T, CODE>) {
+    // codes that no row sees count as zero, for 0 times NaN is not 0
+    if (!whole) {
 #pragma unroll
       for (int c = 0; c < F::kChannels; ++c) {
         u32x4 w = v16[c];
-        if (!whole) {
-          w.x = page_ok ? keep_tokens(w.x, t_lane, lo, hi) : 0u;
-          w.y = page_ok ? keep_tokens(w.y, t_lane + 4, lo, hi) : 0u;
-          w.z = page_ok ? keep_tokens(w.z, t_lane + 8, lo, hi) : 0u;
-          w.w = page_ok ? keep_tokens(w.w, t_lane + 12, lo, hi) : 0u;
-        }
-        if ((p_min != p_max && !all_see(t0)) || kLeaveOut<T, CODE>) {
-          odd = odd || any_unbounded<CODE>(w);
-          w = bounded<CODE>(w);
-        }
+        w.x = page_ok ? keep_tokens(w.x, t_lane, lo, hi) : 0u;
+        w.y = page_ok ? keep_tokens(w.y, t_lane + 4, lo, hi) : 0u;
+        w.z = page_ok ? keep_tokens(w.z, t_lane + 8, lo, hi) : 0u;
+        w.w = page_ok ? keep_tokens(w.w, t_lane + 12, lo, hi) : 0u;
         v16[c] = w;
       }
+    }
+    if constexpr (LEAVE_OUT) {
+#pragma unroll
+      for (int c = 0; c < F::kChannels; ++c) v16[c] = bounded<CODE>(v16[c]);
     }
 
 #pragma unroll
@@ -670,11 +698,10 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
     }
   }
 
-  if (__any(odd)) {  // the rows that see such a value get it
+  if constexpr (LEAVE_OUT) {  // the rows that see such a value get it
 #pragma unroll 1
     for (step = begin + wave; step < end; step += F::kWaves) {
       const int32_t t0 = (int32_t)(step * kStep), t_lane = t0 + value_chunk;
-      if (all_see(t0) && !kLeaveOut<T, CODE>) continue;
       load_values(t0, page_of(t_lane));
 #pragma unroll
       for (int c = 0; c < F::kChannels; ++c) {
@@ -710,7 +737,22 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
       join_ml[wave][16 * n + col][1] = l[n];
     }
   }
+  if constexpr (!LEAVE_OUT) {
+    float sums = 0;
+#pragma unroll
+    for (int n = 0; n < NM; ++n)
+#pragma unroll
+      for (int c = 0; c < F::kChannels; ++c) sums = not_finite(sums, acc[n][c]);
+    const bool odd = __any(sums != 0);
+    if (lane == 0) join_odd[wave] = odd;
+  }
   __syncthreads();
+  if constexpr (!LEAVE_OUT) {
+    uint32_t odd = 0;
+#pragma unroll
+    for (int w = 0; w < F::kWaves; ++w) odd |= join_odd[w];
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(odd), 0)) return false;
+  }
 #pragma unroll
   for (int n = 0; n < NM; ++n) {
     float top = -INFINITY, sum = 0;
@@ -725,7 +767,7 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
     m[n] = top;
     l[n] = sum;
 #pragma unroll
-    for (int c = 0; c < F::kChannels; ++c) acc[n][c] *= shrink;
+    for (int c = 0; c < F::kChannels; ++c) acc[n][c] = LEAVE_OUT ? weighed(acc[n][c], shrink) : acc[n][c] * shrink;
   }
 #pragma unroll
   for (int half = 2; half >= 1; half >>= 1) {
@@ -742,7 +784,7 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
         for (int c = 0; c < F::kChannels; ++c) acc[n][c] += *(const f32x4 *)&join_acc[wave][16 * n + col][16 * c + 4 * g];
     __syncthreads();
   }
-  if (wave != 0) return;
+  if (wave != 0) return true;
 #pragma unroll
   for (int n = 0; n < NM; ++n) {
     const uint32_t in = 16 * n + col, r = r0 + in;
@@ -764,6 +806,18 @@ __device__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index
     for (int c = 0; c < F::kChannels; ++c) store4<T>(out + 16 * c + 4 * g, acc[n][c] * inv, a.out_vec);
     if (a.lse && g == 0) a.lse[row * a.n_q_heads + head] = l[n] == 0 ? -INFINITY : (m[n] + log2_fast(l[n])) * 0.6931471805599453f;
   }
+  return true;
+}
+
+template <int T, int CODE, int D, int NM>
+__device__ __forceinline__ void few_rows(const AttendArgs &a, const Lists &lists, uint32_t index) {
+  typedef FewRows<D, NM> F;
+  __shared__ float join_acc[2][F::kRows][D + 4];
+  __shared__ float join_ml[F::kWaves][F::kRows][2];
+  __shared__ uint32_t join_odd[F::kWaves];  // a NaN or an infinity was met
+  const bool done = few_rows_piece<T, CODE, D, NM, false>(a, lists, index, join_acc, join_ml, join_odd);
+  if (__builtin_expect(!__builtin_amdgcn_readfirstlane(done), 0))
+    few_rows_piece<T, CODE, D, NM, true>(a, lists, index, join_acc, join_ml, join_odd);
 }
 
 // ------------------------------------------------------------------ many rows
@@ -822,7 +876,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
   __shared__ u32x4 values[F::kRing][F::kAll];
   __shared__ float key_scale[F::kRing][4], value_scale[F::kRing][4];  // of 16 tokens each; a key's is -1 where there is no page
   __shared__ int32_t step_page[F::kPages][4];        // pages of 16 tokens each
-  __shared__ uint32_t odd;                              // a NaN or an infinity was left out
+  __shared__ uint32_t odd;                           // a NaN or an infinity was met
   Piece pc;
   if (!find_piece<F::kThreads, false>(a, lists, index, &pc)) return;
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
@@ -850,9 +904,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
     for (int s = 0; s < kKeySteps; ++s) query_frag<T>(x + 32 * (s / 2) + 16 * half + 8 * (s % 2), a.q_vec, a.negate, &q[s]);
   }
   f32x16 acc[kChannels];
-#pragma unroll
-  for (int c = 0; c < kChannels; ++c) acc[c] = f32x16{};
-  float m = -INFINITY, l = 0;
+  float m, l;
 
   // staging: thread's chunks n = tid + 256 i
   const int32_t *table = a.table + (size_t)pc.req * a.max_pages;
@@ -913,7 +965,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
     }
     if (tid < 4) next_page = page_of(t0 + kStep + 16 * (int32_t)tid);
   };
-  auto put_one = [&](uint32_t b, int32_t t, bool edge, bool gaps, uint32_t n, const u32x4 &k, u32x4 w) {
+  auto put_one = [&](auto leave_out, uint32_t b, int32_t t, bool edge, bool gaps, uint32_t n, const u32x4 &k, u32x4 w) {
     if (!F::has(n)) return;
     keys[b][F::key_at(n / F::kChunks, n % F::kChunks)] = k;
     if (edge || gaps) {  // codes that no row sees count as zero, for 0 times NaN is not 0
@@ -922,17 +974,14 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
       w.z = stage_ok ? keep_tokens(w.z, t + 8, lo, hi) : 0u;
       w.w = stage_ok ? keep_tokens(w.w, t + 12, lo, hi) : 0u;
     }
-    if (edge || kLeaveOut<T, CODE>) {
-      if (any_unbounded<CODE>(w)) odd = 1;  // seen by some rows perhaps: left for after the loop
-      w = bounded<CODE>(w);
-    }
+    if constexpr (leave_out) w = bounded<CODE>(w);
     values[b][F::value_at(n / 4, n % 4)] = w;
   };
-  auto put = [&](uint32_t step) {
+  auto put = [&](auto leave_out, uint32_t step) {
     const uint32_t b = step % F::kRing;
     const int32_t t0 = (int32_t)(step * kStep), t = t0 + 16 * (int32_t)(tid % 4);
     const bool edge = !all_see(t0), gaps = !__all(stage_ok);
-    static_for<F::kLoads>([&](auto i) { put_one(b, t, edge, gaps, tid + F::kThreads * i, stage_k[i], stage_v[i]); });
+    static_for<F::kLoads>([&](auto i) { put_one(leave_out, b, t, edge, gaps, tid + F::kThreads * i, stage_k[i], stage_v[i]); });
     if (tid < 4) {
       key_scale[b][tid] = exp_ok ? pow2((int)stage_exp) : -1.0f;
       step_page[(step + 1) % F::kPages][tid] = next_page;
@@ -941,110 +990,123 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
     }
   };
   if (tid == 0) odd = 0;
-  if (tid < 4) step_page[begin % F::kPages][tid] = page_of((int32_t)(begin * kStep) + 16 * (int32_t)tid);
-  __syncthreads();
-  if (begin < end) {
-    load(begin);
-    put(begin);
-  }
-  __syncthreads();
   const uint32_t key_row = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);  // token of this lane's row
-  for (uint32_t step = begin; step < end; ++step) {
-    const uint32_t b = step % F::kRing;
-    const int32_t t0 = (int32_t)(step * kStep);
-    if (step + 1 < end) load(step + 1);
-    if (w0 < list && t0 <= p_max && (a.window == 0 || (int64_t)t0 + kStep - 1 > (int64_t)p_min - a.window)) {
-      f32x16 s[kTiles];
-      // The scores' products are issued before the other waves' softmax, which fills
-      // the gaps between them (with it 703 us, without 717, a prompt of 8192).
-      __builtin_amdgcn_s_setprio(1);
+  auto sum_up = [&](auto leave_out) {  // m, l and acc over all steps, without codes that are not finite or with them
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        s[i] = f32x16{};
-#pragma unroll
-        for (int c = 0; c < kChannels; ++c) {
-          const u32x4 w = keys[b][F::key_at(32 * i + key_row, 2 * c + half)];
-          s[i] = score_mfma32<T>(key_frag<T, CODE>(w.x, w.y), q[2 * c], s[i]);
-          s[i] = score_mfma32<T>(key_frag<T, CODE>(w.z, w.w), q[2 * c + 1], s[i]);
-        }
-      }
-      __builtin_amdgcn_s_setprio(0);
-      static_assert(kTiles == 2, "two scales to a lane's part of a step");
-      float ks[kTiles], vs[kTiles];  // ks: what a score is still to be multiplied by
-      bool page_ok[kTiles], pages_ok = true;
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        const float x = key_scale[b][2 * i + half];
-        page_ok[i] = x >= 0;
-        pages_ok = pages_ok && page_ok[i];
-        ks[i] = x * a.scale_log2;
-        vs[i] = value_scale[b][2 * i + half];
-      }
-      const bool whole = t0 + kStep - 1 <= p_min && (a.window == 0 || (int64_t)t0 > (int64_t)p_max - a.window) && __all(pages_ok);
-      if (!whole) {
+    for (int c = 0; c < kChannels; ++c) acc[c] = f32x16{};
+    m = -INFINITY;
+    l = 0;
+    if (tid < 4) step_page[begin % F::kPages][tid] = page_of((int32_t)(begin * kStep) + 16 * (int32_t)tid);
+    __syncthreads();
+    if (begin < end) {
+      load(begin);
+      put(leave_out, begin);
+    }
+    __syncthreads();
+    for (uint32_t step = begin; step < end; ++step) {
+      const uint32_t b = step % F::kRing;
+      const int32_t t0 = (int32_t)(step * kStep);
+      if (step + 1 < end) load(step + 1);
+      if (w0 < list && t0 <= p_max && (a.window == 0 || (int64_t)t0 + kStep - 1 > (int64_t)p_min - a.window)) {
+        f32x16 s[kTiles];
+        // The scores' products are issued before the other waves' softmax, which fills
+        // the gaps between them (with it 703 us, without 717, a prompt of 8192).
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
+          s[i] = f32x16{};
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            s[i][j] = page_ok[i] && sees(seen, t0 + 32 * i + 16 * (int32_t)half + j) ? s[i][j] * ks[i] : -INFINITY;
-          ks[i] = 1;
-        }
-      }
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        float t = s[i][0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) t = fmaxf(t, s[i][j]);
-        top = fmaxf(top, t * ks[i]);
-      }
-      if (__any(top > m + lag_for(fmaxf(vs[0], vs[1])))) {
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m2 = fmaxf(m, top);
-        const float shrink = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
-        m = m2;
-        l *= shrink;
-#pragma unroll
-        for (int c = 0; c < kChannels; ++c) acc[c] *= shrink;
-      }
-      const float base = m == -INFINITY ? 0.0f : m;
-      Frag p[kTiles][2][PROBS];
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          float x = exp2_fast(__builtin_fmaf(s[i][j], ks[i], -base));
-          l += x;
-#pragma unroll
-          for (int t = 0; t < PROBS; ++t) {
-            p[i][j / 8][t].b[j % 8] = (__bf16)x;
-            if (t + 1 < PROBS) x -= (float)p[i][j / 8][t].b[j % 8];
+          for (int c = 0; c < kChannels; ++c) {
+            const u32x4 w = keys[b][F::key_at(32 * i + key_row, 2 * c + half)];
+            s[i] = score_mfma32<T>(key_frag<T, CODE>(w.x, w.y), q[2 * c], s[i]);
+            s[i] = score_mfma32<T>(key_frag<T, CODE>(w.z, w.w), q[2 * c + 1], s[i]);
           }
         }
+        __builtin_amdgcn_s_setprio(0);
+        static_assert(kTiles == 2, "two scales to a lane's part of a step");
+        float ks[kTiles], vs[kTiles];  // ks: what a score is still to be multiplied by
+        bool page_ok[kTiles], pages_ok = true;
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i)
+        for (int i = 0; i < kTiles; ++i) {
+          const float x = key_scale[b][2 * i + half];
+          page_ok[i] = x >= 0;
+          pages_ok = pages_ok && page_ok[i];
+          ks[i] = x * a.scale_log2;
+          vs[i] = value_scale[b][2 * i + half];
+        }
+        const bool whole = t0 + kStep - 1 <= p_min && (a.window == 0 || (int64_t)t0 > (int64_t)p_max - a.window) && __all(pages_ok);
+        if (!whole) {
 #pragma unroll
-        for (int c = 0; c < kChannels; ++c) {
-          const u32x4 w = values[b][F::value_at(32 * c + col, 2 * i + half)];
+          for (int i = 0; i < kTiles; ++i) {
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const Frag v = u ? codes_bf16<CODE>(w.z, w.w, vs[i]) : codes_bf16<CODE>(w.x, w.y, vs[i]);
-#pragma unroll
-            for (int t = PROBS - 1; t >= 0; --t)
-              acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.b, p[i][u][t].b, acc[c], 0, 0, 0);
+            for (int j = 0; j < 16; ++j)
+              s[i][j] = page_ok[i] && sees(seen, t0 + 32 * i + 16 * (int32_t)half + j) ? s[i][j] * ks[i] : -INFINITY;
+            ks[i] = 1;
           }
         }
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          float t = s[i][0];
+#pragma unroll
+          for (int j = 1; j < 16; ++j) t = fmaxf(t, s[i][j]);
+          top = fmaxf(top, t * ks[i]);
+        }
+        if (__any(top > m + lag_for(fmaxf(vs[0], vs[1])))) {
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float m2 = fmaxf(m, top);
+          const float shrink = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
+          m = m2;
+          l *= shrink;
+#pragma unroll
+          for (int c = 0; c < kChannels; ++c) acc[c] *= shrink;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+        Frag p[kTiles][2][PROBS];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            float x = exp2_fast(__builtin_fmaf(s[i][j], ks[i], -base));
+            l += x;
+#pragma unroll
+            for (int t = 0; t < PROBS; ++t) {
+              p[i][j / 8][t].b[j % 8] = (__bf16)x;
+              if (t + 1 < PROBS) x -= (float)p[i][j / 8][t].b[j % 8];
+            }
+          }
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int c = 0; c < kChannels; ++c) {
+            const u32x4 w = values[b][F::value_at(32 * c + col, 2 * i + half)];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const Frag v = u ? codes_bf16<CODE>(w.z, w.w, vs[i]) : codes_bf16<CODE>(w.x, w.y, vs[i]);
+#pragma unroll
+              for (int t = PROBS - 1; t >= 0; --t)
+                acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.b, p[i][u][t].b, acc[c], 0, 0, 0);
+            }
+          }
+      }
+      // the other slot was last read in the step before, which every wave has left
+      if (step + 1 < end) put(leave_out, step + 1);
+      __syncthreads();
     }
-    // the other slot was last read in the step before, which every wave has left
-    if (step + 1 < end) put(step + 1);
-    __syncthreads();
-  }
-
-  if (odd) {  // the rows that see a value left out get it
+  };
+  sum_up(std::false_type{});
+  float sums = 0;
+#pragma unroll
+  for (int c = 0; c < kChannels; ++c)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sums = __builtin_fmaf(acc[c][j], 0.0f, sums);
+  if (sums != 0) odd = 1;
+  __syncthreads();
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(odd), 0)) {  // without it, and the rows that see such a value get it
+    sum_up(std::true_type{});
 #pragma unroll 1
     for (uint32_t step = begin; step < end; ++step) {
       const int32_t t0 = (int32_t)(step * kStep);
-      if (all_see(t0) && !kLeaveOut<T, CODE>) continue;
 #pragma unroll
       for (int c = 0; c < kChannels; ++c)
 #pragma unroll 1
@@ -1129,11 +1191,15 @@ __device__ void join_rows(const AttendArgs &a, const Lists &lists, bool last_fir
     for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
     f32x4 acc = {0, 0, 0, 0};
     float l = 0;
+    auto weight = [&](size_t at) {
+      const float ms = ml[2 * at];
+      return ms == m ? 1.0f : exp2_fast(ms - m);
+    };
     if (group < kGroups) {
 #pragma unroll 4
       for (uint32_t s = group; s < pc.splits; s += kGroups) {
         const size_t at = (size_t)s * rows;
-        const float ms = ml[2 * at], w = ms == m ? 1.0f : exp2_fast(ms - m);
+        const float w = weight(at);
         l += w * ml[2 * at + 1];
         acc += w * *(const f32x4 *)(accs + at * D);
       }
@@ -1144,6 +1210,14 @@ __device__ void join_rows(const AttendArgs &a, const Lists &lists, bool last_fir
       l += __shfl(l, from);
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[j] += __shfl(acc[j], from);
+    }
+    if (__builtin_expect(__any(not_finite(0, acc) != 0), 0)) {  // a weight of 0 on an infinity, perhaps
+      acc = f32x4{0, 0, 0, 0};
+#pragma unroll 1
+      for (uint32_t s = 0; s < pc.splits; ++s) {
+        const size_t at = (size_t)s * rows;
+        if (group == 0) acc += weighed(*(const f32x4 *)(accs + at * D), weight(at));
+      }
     }
     if (group != 0) continue;
     const int64_t row = pc.q.first + (int64_t)(r / a.group), head = (int64_t)pc.head * a.group + r % a.group;

@@ -99,3 +99,23 @@ def test_attend_values_near_the_end_of_32_bits(uz, fmt, kind, total, new):
         want, got = side.attend(uz, kind, new)
         assert np.isfinite(want["out"]).all() and np.abs(want["out"]).max() > 1e34
         check_attend(got, want, kind, 64, total)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("total,new,window", [(300, 1, 0), (321, 9, 0), (530, 200, 0), (530, 200, 450), (3000, 1, 0), (9000, 170, 0)])
+def test_attend_infinity_at_a_weight_below_32_bits(uz, kind, total, new, window):
+    """An infinite value is infinite for every row that sees it, also where its weight of e^-256 is 0 in 32 bits, and
+    whichever step, wave or piece it falls in."""
+    say("infinity", kind, total, new, window)
+    for most in (90, 130, 259, total - new - 3):                          # the token that has all the weight
+        side = Scored(uz, "e5m2", total, 64, {most: 256.0})
+        for t, ch, x in [(5, 3, "inf"), (89, 4, "-inf"), (91, 8, "inf"), (200, 5, "inf"), (201, 5, "-inf"), (270, 9, "-inf"),
+                         (total - 1, 6, "inf"), (100, 7, "nan"), (total - new, 10, "inf"), (total // 2, 11, "-inf")]:
+            side.value(t, ch, float(x))
+        want, (out, lse) = side.attend(uz, kind, new, window)
+        got, fine = np_of(out), np.isfinite(want["out"])
+        assert not fine.all() and fine.any()
+        assert np.array_equal(got[~fine], want["out"][~fine], equal_nan=True)
+        assert np.isfinite(got[fine]).all()
+        clean = {k: np.where(fine, v, 0.0) if k in ("out", "spread") else v for k, v in want.items()}
+        check_attend((torch.from_numpy(np.where(fine, got, 0.0)), lse), clean, kind, 64, total)
