@@ -167,6 +167,14 @@ __device__ __forceinline__ uint32_t piece_steps(const AttendArgs &a, const Lists
   return (uint32_t)min((steps + pieces - 1) / pieces, (uint64_t)INT32_MAX);
 }
 
+// Pieces and slots are added up in one word, pieces in the low bits.  Row starts that do
+// not ascend make requests share rows, so that each may have all blocks; slots stay
+// below twice the pieces that piece_steps aims at.
+constexpr int kPieceBits = 40;
+static_assert((UZIP_KV_MAX_REQUESTS + 1) * (UZIP_KV_MAX_ROW_HEADS / 16 + 1024ull) + 2 * kFewPieces * kMostUnits < 1ull << kPieceBits,
+              "the pieces of all requests");
+static_assert(2 * kFewPieces * kMostUnits < 1ull << (64 - kPieceBits) && many_pieces(64) <= kFewPieces, "their slots");
+
 // Which piece of the lists is number `index`, found by the whole workgroup.  A block
 // of n steps is split only where n > S = piece_steps, into ceil(n / S) < 2 n / S pieces:
 // with at most k units of pieces' worth of steps, k = kFewPieces or many_pieces, there are at
@@ -215,7 +223,7 @@ __device__ bool find_piece(const AttendArgs &a, const Lists &lists, uint32_t ind
     const uint32_t n = steps_of(a, q, rows);
     *splits = n > length ? (n + length - 1) / length : 1u;
     const uint64_t pieces = (uint64_t)b * a.c.heads * (JOIN ? (*splits > 1 ? 1u : 0u) : *splits);
-    return pieces | (*splits > 1 ? (uint64_t)b * a.c.heads * *splits : 0) << 32;  // pieces; slots
+    return pieces | (*splits > 1 ? (uint64_t)b * a.c.heads * *splits : 0) << kPieceBits;
   };
   uint64_t mine = 0;
   uint32_t splits;
@@ -229,12 +237,14 @@ __device__ bool find_piece(const AttendArgs &a, const Lists &lists, uint32_t ind
     if (w < (int)wave) at += part[2 * kWaves + w];
     total += part[2 * kWaves + w];
   }
-  if (index >= (uint32_t)total) return false;
+  constexpr uint64_t kPieces = (1ull << kPieceBits) - 1;
+  if (index >= (total & kPieces)) return false;
   for (uint32_t i = lo; i < hi; ++i) {
     const Request q = request_at(i);
     const uint64_t c = count(q, &splits);
-    const uint32_t rest = index - (uint32_t)at;
-    if (index >= (uint32_t)at && rest < (uint32_t)c) {
+    const uint64_t before = at & kPieces;
+    if (index >= before && index - before < (c & kPieces)) {
+      const uint32_t rest = index - (uint32_t)before;
       Piece p;
       p.q = q;
       p.req = i;
@@ -243,7 +253,7 @@ __device__ bool find_piece(const AttendArgs &a, const Lists &lists, uint32_t ind
       p.split = JOIN ? 0 : up % splits;
       p.splits = splits;
       p.block = JOIN ? up : up / splits;
-      p.part = lists.slots + ((at >> 32) + (uint64_t)(p.block * a.c.heads + p.head) * splits) * rows;
+      p.part = lists.slots + ((at >> kPieceBits) + (uint64_t)(p.block * a.c.heads + p.head) * splits) * rows;
       found = p;
     }
     at += c;

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import kv as ref
-from test_gpu_kv import Side, check_attend, dev, ints, np_of, rows_of, run_attend, say, uz  # noqa: F401
+from test_gpu_kv import Side, TYPES, check_attend, dev, ints, np_of, rows_of, run_attend, say, uz  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -119,3 +119,37 @@ def test_attend_infinity_at_a_weight_below_32_bits(uz, kind, total, new, window)
         assert np.isfinite(got[fine]).all()
         clean = {k: np.where(fine, v, 0.0) if k in ("out", "spread") else v for k, v in want.items()}
         check_attend((torch.from_numpy(np.where(fine, got, 0.0)), lse), clean, kind, 64, total)
+
+
+# ------------------------------------------------------------------ attention: memory beside the outputs
+def between_guards(shape, dtype, fill=77):
+    """A contiguous tensor with 4096 guard bytes before and behind it, and a check of them."""
+    size = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+    room = torch.full((size + 8192,), fill, dtype=torch.uint8, device="cuda")
+
+    def check():
+        assert (room[:4096] == fill).all() and (room[4096 + size:] == fill).all()
+    return room[4096:4096 + size].view(dtype).view(shape), check
+
+
+@pytest.mark.parametrize("starts", [[0, 300, 0, 300, 0, 300], [300, 200, 100, 50, 20, 0], [-5, 2 ** 31 - 1, -2 ** 31, 7, 7, 301],
+                                    [0, 0, 0, 0, 0, 0], [299, 299, 300, 2 ** 30, 0, 1]], ids=str)
+@pytest.mark.parametrize("kind,dim,heads", [("bf16", 128, 8), ("fp16", 64, 2), ("fp32", 96, 4)])
+def test_attend_writes_only_its_outputs_whatever_the_row_starts(uz, kind, dim, heads, starts):
+    """Row starts that descend, repeat, share rows or lie outside: nothing beside out, lse and workspace is written."""
+    say("row starts", starts, kind, dim)
+    g = np.random.default_rng(95)
+    side = Side(uz, 40, 1, 64, dim, "e4m3fn", g)
+    q, qd = rows_of((300, heads, dim), kind, g)
+    for lens in ([2500, 2500, 700, 2 ** 31 - 1, -4], [300] * 5):
+        out, out_fine = between_guards((300, heads, dim), TYPES[kind])
+        lse, lse_fine = between_guards((300, heads), torch.float32)
+        for most in (1, 60, 300):
+            ws, ws_fine = between_guards((uz.uzip_kv_attend_workspace({"bf16": 0, "fp16": 1, "fp32": 2}[kind], 300, heads, 1, dim, 5, most),),
+                                         torch.uint8)
+            table = torch.randint(-1, 40, (5, 40), dtype=torch.int32, device="cuda")
+            uz.kv_attend(qd, side.cache, table, ints(lens), ints(starts), most, out=out, lse=lse, ws=ws)
+            torch.cuda.synchronize()
+            out_fine()
+            lse_fine()
+            ws_fine()
