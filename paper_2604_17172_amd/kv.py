@@ -97,7 +97,8 @@ class KVPlan:
     __slots__ = ("requests", "rows", "page_tokens", "lens", "q_start", "slots", "runs", "counts", "status", "_ptrs")
 
     def __init__(self, requests: int, rows: int, page_tokens: int, device="cuda"):
-        runs = uzip_kv_max_runs(rows, requests, page_tokens) if rows >= 0 and requests >= 0 else 0
+        fits = 0 <= rows <= KV_MAX_ROWS and 0 <= requests <= KV_MAX_REQUESTS and 0 <= page_tokens < 1 << 32
+        runs = uzip_kv_max_runs(rows, requests, page_tokens) if fits else 0
         if runs == 0:
             _check(EINVAL, "uzip_kv_max_runs")
 
@@ -151,7 +152,8 @@ def kv_plan(old: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: tor
     if out is None:
         with _on(stream):
             out = KVPlan(n, rows, page_tokens, old.device)
-    elif n > out.requests or not 0 <= rows <= out.rows or page_tokens < out.page_tokens or out.lens.get_device() != device:
+    elif (n > out.requests or not 0 <= rows <= out.rows or not out.page_tokens <= page_tokens < 1 << 32
+          or out.lens.get_device() != device):
         raise ValueError("out is for fewer requests or rows, larger pages or another GPU")
     rc = uzip_kv_plan(old.data_ptr(), new.data_ptr(), n, free.data_ptr(), free.numel(), page_tokens, rows, table.data_ptr(),
                       table.shape[1], *out._ptrs, _handle(stream, device))
