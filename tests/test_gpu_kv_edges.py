@@ -153,3 +153,63 @@ def test_attend_writes_only_its_outputs_whatever_the_row_starts(uz, kind, dim, h
             out_fine()
             lse_fine()
             ws_fine()
+
+
+# ------------------------------------------------------------------ attention: pieces longer than the least
+def check_sampled(uz, kind, dim, kv, group, fmt, page, ctx, new, seed, window=0):
+    """All requests read pages of one small pool; out, lse and a workspace of just its size lie between guards; a few rows of
+    each of a few requests are compared."""
+    g = np.random.default_rng(seed)
+    most = max(c + n for c, n in zip(ctx, new))
+    pages = -(-most // page) + 7
+    side = Side(uz, pages, kv, page, dim, fmt, g)
+    finite = np.arange(256, dtype=np.uint8)[np.isfinite(ref.code_values(fmt)) & (np.abs(ref.code_values(fmt)) < 8)]
+    side.k, side.v = finite[side.k % len(finite)], finite[side.v % len(finite)]
+    side.k_exp[:], side.v_exp[:] = g.integers(124, 129, side.k_exp.shape), g.integers(124, 129, side.v_exp.shape)
+    for mine, its in ((side.k, side.cache.k), (side.v.transpose(0, 1, 3, 2), side.cache.v), (side.k_exp, side.cache.k_exp),
+                      (side.v_exp, side.cache.v_exp)):
+        its.copy_(dev(mine))
+    table = np.stack([g.permutation(pages)[:pages - 6] for _ in ctx]).astype(np.int32)
+    lens = np.array([c + n for c, n in zip(ctx, new)], np.int32)
+    starts = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    rows, heads = sum(new), kv * group
+    q, qd = rows_of((rows, heads, dim), kind, g)
+    out, out_fine = between_guards((rows, heads, dim), TYPES[kind])
+    lse, lse_fine = between_guards((rows, heads), torch.float32)
+    ws, ws_fine = between_guards((uz.kv_attend_workspace(qd, side.cache, len(ctx), max(new)).numel(),), torch.uint8, fill=255)
+    ws.fill_(255)
+    scale = dim ** -0.5
+    uz.kv_attend(qd, side.cache, ints(table), ints(lens), ints(starts), max(new), scale=scale, window=window, out=out, lse=lse, ws=ws)
+    torch.cuda.synchronize()
+    out_fine()
+    lse_fine()
+    ws_fine()
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    for i in sorted({0, len(ctx) - 1, *g.integers(0, len(ctx), 3).tolist()}):
+        for j in sorted({0, new[i] - 1, *g.integers(0, new[i], 3).tolist()}):
+            r, length = int(starts[i]) + j, ctx[i] + j + 1                # the row as the last of a shorter request
+            want = ref.attend(np_of(q[r:r + 1]), side.k, side.k_exp, side.v, side.v_exp, fmt, table[i:i + 1], [length], [0, 1], page,
+                              scale, window)
+            check_attend((out[r:r + 1], lse[r:r + 1]), want, kind, dim, length)
+
+
+@pytest.mark.parametrize("kind,dim,kv,group,ctx,new", [
+    ("bf16", 128, 8, 1, [14000], [520]),                                  # 40 blocks of 228 steps: pieces of 18
+    ("fp16", 64, 8, 2, [14000, 9000], [300, 201]),                        # 72 blocks: pieces of 13 or 14
+    ("bf16", 96, 4, 3, [60000, 100, 3], [200, 1, 180]),                   # long and short lists in one call
+    ("fp16", 256, 2, 4, [20000, 20], [240, 40]),
+    ("bf16", 192, 2, 4, [20000, 777], [400, 3]),
+])
+def test_attend_long_pieces_of_many_rows(uz, kind, dim, kv, group, ctx, new):
+    say("long pieces", kind, dim, kv, group, ctx, new)
+    check_sampled(uz, kind, dim, kv, group, "e4m3fn", 64, ctx, new, 96)
+    check_sampled(uz, kind, dim, kv, group, "e5m2", 16, ctx, new, 97, window=9000)
+
+
+@pytest.mark.parametrize("kind,dim,group", [("bf16", 128, 4), ("fp16", 64, 7), ("fp32", 96, 1), ("bf16", 64, 20), ("fp32", 256, 2)])
+def test_attend_long_pieces_of_few_rows(uz, kind, dim, group):
+    """More than 32768 steps in all: four pieces for a compute unit are longer than 32 steps."""
+    say("long few", kind, dim, group)
+    ctx = [5000 + 101 * i for i in range(64)]
+    check_sampled(uz, kind, dim, 8, group, "e4m3fn", 64, ctx, [1] * 64, 98)
+    check_sampled(uz, kind, dim, 8, group, "e5m2", 128, ctx, [1] * 40 + [2] * 24, 99, window=7777)
