@@ -508,9 +508,11 @@ __device__ __forceinline__ bool few_rows_piece(const AttendArgs &a, const Lists 
   Piece pc;
   if (!find_piece<F::kThreads, false>(a, lists, index, &pc)) return true;
   const uint32_t lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  // one number for a wave in blocks of 32, whose registers are short (dim 128: 73 us, else
-  // 82), but not in blocks of 16 (64 requests, dim 128: 106 us, without 104)
-  const uint32_t wave = NM == 2 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x >> 6;
+  // One number for a wave, which saves a few registers (16 requests of 4000 tokens, 72 rows:
+  // dim 96 36 us, else 42, for a third workgroup fits a compute unit; 256 99 and 104; blocks of
+  // 32, dim 128: 73 and 82), but not in blocks of 16 of dim 128 (64 requests: 106, without 104).
+  constexpr bool kOneNumber = NM == 2 || D != 128;
+  const uint32_t wave = kOneNumber ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x >> 6;
   const uint32_t list = (uint32_t)pc.q.rows * a.group, r0 = pc.block * F::kRows, P = a.c.page;
   int32_t lo, hi;
   seen_range(a, pc.q, r0, min(list, r0 + F::kRows), &lo, &hi);
