@@ -92,9 +92,10 @@ class KVCache:
 class KVPlan:
     """A step's places, on the GPU (see uzip_kv_plan), for up to ``requests`` requests and ``rows`` new tokens: lens
     int32 [requests], q_start int32 [requests + 1], slots int64 [rows], runs int32 [max runs, 2], counts int32 [2]
-    (pages taken, runs), status int32 [1] (of the last call)."""
+    (pages taken, runs), status int32 [1] (of the last call).  After a call with fewer requests or rows, lens, q_start
+    and slots are the parts that it wrote."""
 
-    __slots__ = ("requests", "rows", "page_tokens", "lens", "q_start", "slots", "runs", "counts", "status", "_ptrs")
+    __slots__ = ("requests", "rows", "page_tokens", "lens", "q_start", "slots", "runs", "counts", "status", "_ptrs", "_all")
 
     def __init__(self, requests: int, rows: int, page_tokens: int, device="cuda"):
         fits = 0 <= rows <= KV_MAX_ROWS and 0 <= requests <= KV_MAX_REQUESTS and 0 <= page_tokens < 1 << 32
@@ -108,7 +109,13 @@ class KVPlan:
         self.lens, self.q_start, self.slots = new(requests), new(requests + 1), new(rows, dtype=torch.int64)
         self.runs, self.counts = new(runs, 2), new(2)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self._all = self.lens, self.q_start, self.slots
         self._ptrs = tuple(t.data_ptr() for t in (self.lens, self.q_start, self.slots, self.runs, self.counts, self.status))
+
+    def _narrow(self, requests: int, rows: int) -> None:
+        """What lies past a call's requests and rows is an earlier call's."""
+        lens, q_start, slots = self._all
+        self.lens, self.q_start, self.slots = lens[:requests], q_start[:requests + 1], slots[:rows]
 
 
 def kv_plan_buffers(requests: int, rows: int, page_tokens: int, device="cuda") -> KVPlan:
@@ -159,6 +166,8 @@ def kv_plan(old: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: tor
                       table.shape[1], *out._ptrs, _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_kv_plan")
+    if n != out.lens.numel() or rows != out.slots.numel():
+        out._narrow(n, rows)
     if check:
         (stream or torch.cuda.current_stream()).synchronize()
         _check(int(out.status.item()), "uzip_kv_plan")

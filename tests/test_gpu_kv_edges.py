@@ -47,6 +47,31 @@ def test_each_replay_of_a_plan_has_its_own_status(uz):
         assert int(plan.status.item()) == status, tokens
 
 
+def test_a_plan_used_again_for_fewer_requests_shows_only_theirs(uz):
+    """Eight requests take three tokens each, then five of them one: attention over the plan's lengths sees no request of before."""
+    g = np.random.default_rng(94)
+    side = Side(uz, 16, 1, 16, 64, "e4m3fn", g)
+    plan = uz.kv_plan_buffers(8, 24, 16)
+    free, table = ints(np.arange(16)), ints(np.full((8, 2), -1))
+    uz.kv_plan(ints([0] * 8), ints([3] * 8), free, table, 16, 24, out=plan, check=True)
+    k, kd = rows_of((24, 1, 64), "bf16", g)
+    v, vd = rows_of((24, 1, 64), "bf16", g)
+    uz.kv_store(side.cache, kd, vd, plan.slots, plan.runs, plan.counts)
+    side.store(np_of(k), np_of(v), plan.slots.tolist(), [(3 * i, 3) for i in range(8)])
+    uz.kv_plan(ints([3] * 5), ints([1] * 5), free, table[:5], 16, 5, out=plan, check=True)
+    assert plan.lens.tolist() == [4] * 5 and plan.q_start.tolist() == list(range(6)) and plan.slots.shape == (5,)
+    k, kd = rows_of((5, 1, 64), "bf16", g)
+    v, vd = rows_of((5, 1, 64), "bf16", g)
+    uz.kv_store(side.cache, kd, vd, plan.slots, plan.runs, plan.counts)
+    side.store(np_of(k), np_of(v), plan.slots.tolist(), [(i, 1) for i in range(5)])
+    q, qd = rows_of((5, 2, 64), "bf16", g)
+    want = ref.attend(np_of(q), side.k, side.k_exp, side.v, side.v_exp, "e4m3fn", table.cpu().numpy(), [4] * 5, range(6), 16, 0.3)
+    got = uz.kv_attend(qd, side.cache, table, plan.lens, plan.q_start, 1, scale=0.3)
+    check_attend(got, want, "bf16", 64, 4)
+    uz.kv_plan(ints([4] * 8), ints([2] * 8), free, table, 16, 24, out=plan, check=True)
+    assert plan.lens.tolist() == [6] * 8 and plan.q_start.tolist() == list(range(0, 18, 2)) and plan.slots.shape == (24,)
+
+
 # ------------------------------------------------------------------ attention: chosen scores and values
 class Scored(Side):
     """One request of `total` tokens, one head: token t scores scores[t] (else 0) for a query that is 1 in channel 0."""
