@@ -108,8 +108,9 @@ uzip_status uzip_kv_plan(const int32_t *d_old, const int32_t *d_new, uint32_t n_
  * 0x7F with the value's sign; an infinity too in e4m3fn, which has none, and
  * the infinity in e5m2.
  *   d_slots, d_runs, d_counts: as uzip_kv_plan makes them; max_runs: entries of
- *                d_runs.  Rows of a run have consecutive slots in one page, and
- *                no two runs of one call share a page.
+ *                d_runs, whose number chooses the kernel.  Rows of a run have
+ *                consecutive slots in one page, and no two runs of one call share
+ *                a page.
  * Errors: EINVAL, EHIP, EUNSUPPORTED. */
 uzip_status uzip_kv_store(const uzip_kv_cache *cache, uzip_dtype dtype, const void *d_k, int64_t k_row,
                           int64_t k_head, const void *d_v, int64_t v_row, int64_t v_head, uint32_t n_rows,

@@ -57,10 +57,12 @@ __device__ __forceinline__ float lag_for(float value_scale) { return value_scale
 
 // Lists of more rows than this go to the many-rows kernel, in blocks of 128.  By few
 // and by many rows, us, in bf16 (16 heads over 4):
-//   16 requests of 4000 tokens, 72 rows: dim 64 27 and 35, 96 29 and 48, 128 42 and 50,
-//   256 83 and 91; 32 of 96 rows: 128 78 and 75, 256 164 and 154; 16 of 160 rows: 64 38
-//   and 42, 96 44 and 64, 192 72 and 116; 16 of 256: 64 49 and 43, 96 56 and 67, 192 101
-//   and 122; but 4 of 60000 tokens, 200 rows: 96 232 and 188, 192 339 and 330.
+//   16 requests of 4000 tokens, 72 rows: dim 64 32 and 36, 96 36 and 50, 128 55 and 52,
+//   256 99 and 107; 32 of 96 rows: 128 98 and 69, 256 200 and 182; 16 of 160 rows: 64 44
+//   and 55, 96 50 and 62, 192 84 and 132; 16 of 256: 64 51 and 57, 96 60 and 65, 192 107
+//   and 136; but 4 of 60000 tokens, 200 rows: 96 174 and 166, 192 370 and 356.
+// So few rows would still be faster up to 256 over some thousand tokens of dim 64, 96 and
+// 192, and many rows from 72 on of dim 128; the lines are for long contexts.
 // fp32 has no such kernel: its three terms make the matrix units the bound, which few
 // rows reach as well.
 constexpr uint32_t kManyRows = 128;
@@ -144,18 +146,18 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
 // How many steps make a piece, from the steps and blocks of all lists.
 //
 // Many rows: two pieces for each compute unit, four of dim 64, whose workgroups are
-// lighter (512 new tokens of dim 64 over 14000: 145 us, by two 165).
+// lighter (512 new tokens of dim 64 over 14000: 159 us, by two 180).
 // Few rows: where there are fewer blocks than compute units, so that about one piece
 // comes to each, and hardly ever a few more, which would be a second round (steps / S +
 // blocks / 2 pieces come of S, more where the blocks are alike): one round of longer
 // pieces beats two of shorter ones, a piece's beginning and end being a few us (a
-// request of 100000 tokens, 8 heads: 49 us, with two to a unit 56; 8 requests of 2000 to
-// 4000 tokens 22.5 and 29.6; 258 pieces where 192 do as well 42 and 32).  Where there
-// are more, or at least half as many as units and long ones (18 requests of 7500 to
-// 30000 tokens, 8 heads of 128, 144 blocks: 147 us, by the rule above 160; of dim 64 76
-// and 111; 20 of 1000 to 4000 of dim 256 by that rule 54, by this one 66), pieces of no
-// less than 32 steps and up to four to a unit, which even out requests of unlike
-// lengths (64 requests of 1 to 8000 tokens: 114 us, with one to a unit 130).
+// request of 100000 tokens, 8 heads: 50 us, with two to a unit 58; 8 requests of 2000 to
+// 4000 tokens 22 and 23, by the rule that follows 26).  Where there are more, or at least
+// half as many as units and long ones (18 requests of 7500 to 30000 tokens, 8 heads of
+// 128, 144 blocks: 144 us, by the rule above 159; of dim 64 74 and 101; 20 of 1000 to 4000
+// of dim 256 by that rule 52, by this one 54), pieces of no less than 32 steps and up to four
+// to a unit, which even out requests of unlike lengths (64 requests of 1 to 8000 tokens:
+// 112 us, with one to a unit 126).
 constexpr uint32_t kFewPieces = 4, kLongPiece = 32;
 constexpr uint32_t many_pieces(uint32_t dim) { return dim == 64 ? 4 : 2; }
 __device__ __forceinline__ uint32_t piece_steps(const AttendArgs &a, const Lists &l, uint64_t steps, uint64_t blocks) {
@@ -289,8 +291,15 @@ __device__ __forceinline__ void static_for(const F &f) {
 // values of row lane % 16; of the second, eight of column lane % 16; of the
 // result, rows 4 (lane / 16) + 0..3 of column lane % 16.  Which place of the
 // contraction a lane's values have is free as long as both operands agree.
+//
+// bf16: the query as it is, probabilities in one bf16 term, 8 bits, as many as the output
+// has.  That takes the error against 64 bits from 1.6e-3, which rounding the output once
+// costs, to 1.9e-3 (64 requests of up to 8191 tokens; a prompt of 8192 1.6e-3 and 2.0e-3).  A
+// second term gives the 1.6e-3, and takes a third more where many rows share the
+// keys: the prompt 862 us for 647, 64 requests of 32 rows 96 for 72; single tokens 116
+// for 115.
 template <int T>
-struct Query {  // bf16: the query as it is, probabilities in one bf16 term
+struct Query {
   static constexpr int kTerms = 1, kProbs = 1;
 };
 template <>
@@ -307,8 +316,10 @@ struct Query<UZIP_FP32> {  // 24 bits: three bf16 terms each
 // of 0, or a later term of a probability, which may be 0 or negative, times it is no
 // infinity, and a factor of 0 on a sum that holds it neither.  A piece is computed as if
 // there were none; if its sums come out not finite, it is computed again with such
-// codes left out, and they are added after that.  A test of every step's codes instead
-// costs up to half (e5m2, dim 128 in blocks of 32: 111 us, this 73; dim 192 61 and 47).
+// codes left out, and they are added after that (with one such value in each request 64
+// requests of up to 8191 tokens 155 us, else 116; a prompt of 8192 856, else 647).  A test of
+// every step's codes instead costs all calls up to half (e5m2, dim 128 in blocks of 32: 111
+// us, this 73; dim 192 61 and 47).
 __device__ __forceinline__ float not_finite(float so_far, f32x4 x) {  // NaN from the first infinity or NaN on, else 0
 #pragma unroll
   for (int j = 0; j < 4; ++j) so_far = __builtin_fmaf(x[j], 0.0f, so_far);
@@ -485,8 +496,8 @@ __device__ __forceinline__ float class_value(int kind) { return kind == 0 ? NAN 
 // Bound by the cache's bytes: the next step's keys are asked for when this one's
 // scores are done, its values after this one's products, so that 16 KiB (dim 128) of
 // each wave are under way.  4 requests of 120000 to 131072 tokens, 8 heads of 128: 1.03
-// GB in 180 us, 5.7 TB/s (a copy of 1 GiB: 5.1 read and written); 64 of up to 8191 and
-// 3 empty ones: 539 MB in 107 us, 5.0 TB/s.  The smallest call, 38 tokens: 6.7 us, of
+// GB in 182 us, 5.6 TB/s (a copy of 1 GiB: 5.1 read and written); 64 of up to 8191 and
+// 3 empty ones: 538 MB in 109 us, 4.9 TB/s.  The smallest call, 38 tokens: 7.1 us, of
 // which 3 are any launch's and the rest a chain of lengths, table, codes and joins.
 template <int D, int NM>
 struct FewRows {
@@ -496,7 +507,7 @@ struct FewRows {
 
 // Without LEAVE_OUT false where a NaN or an infinity was met: then nothing was written,
 // and the piece is computed from its beginning with it, so that nothing is kept in
-// registers for that (a loop around the steps alone: dim 256 102 us, this 78).
+// registers for that (a loop around the steps alone: dim 256 102 us, this 73).
 template <int T, int CODE, int D, int NM, bool LEAVE_OUT>
 __device__ __forceinline__ bool few_rows_piece(const AttendArgs &a, const Lists &lists, uint32_t index,
                                                float (&join_acc)[2][16 * NM][D + 4],
@@ -848,9 +859,9 @@ __device__ __forceinline__ void few_rows(const AttendArgs &a, const Lists &lists
 // others (128 conversions; for each of 32 scores a multiply-add, an exponential, an
 // addition, half a maximum and half a rounding; the rest places and addresses).  Two
 // waves of a SIMD hide a matrix instruction behind about six others, and these take
-// 2 ns each.  A prompt of 8192 tokens, 32 heads over 8 of 128: 625 us, 880 TFLOP/s (a
+// 2 ns each.  A prompt of 8192 tokens, 32 heads over 8 of 128: 637 us, 864 TFLOP/s (a
 // bf16 matrix product of 8192: 1230); counters at that: matrix units 39% busy, vector
-// ALUs 63%.  Slower were: three waves to a SIMD (it spills), codes straight from memory
+// ALUs 64%.  Slower were: three waves to a SIMD (it spills), codes straight from memory
 // to registers (980 us then, with LDS 890), barriers every second step (the same), scores
 // of one tile during the softmax of another (740, 690 without).
 template <int D>
@@ -1022,7 +1033,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
       if (w0 < list && t0 <= p_max && (a.window == 0 || (int64_t)t0 + kStep - 1 > (int64_t)p_min - a.window)) {
         f32x16 s[kTiles];
         // The scores' products are issued before the other waves' softmax, which fills
-        // the gaps between them (with it 703 us, without 717, a prompt of 8192).
+        // the gaps between them (a prompt of 8192 takes 2% longer without).
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
@@ -1179,7 +1190,7 @@ __device__ void many_rows(const AttendArgs &a, const Lists &lists, uint32_t inde
 // Pieces' maxima, sums and accs of the blocks that were split.  A wave takes a row
 // at a time: lanes in groups of dim / 4, four channels to a lane, each group every
 // so many pieces; `part` tells which 16 rows of the block.  Bound by latency: 6 us where
-// nothing was split, 7 for 32 blocks of 15 pieces, 14 for 144 blocks of 128 rows (a
+// little was split, 8 for 32 blocks of 15 pieces, 14 for 144 blocks of 128 rows (a
 // wave's four rows at once took 22: where a block has few rows it loads them again).
 constexpr uint32_t kJoinRows = 16;
 template <int T, int D>
@@ -1242,15 +1253,15 @@ __device__ void join_rows(const AttendArgs &a, const Lists &lists, bool last_fir
 // ------------------------------------------------------------------ kernels
 // Blocks of 32 rows read a list's tokens once where blocks of 16 read them twice, the
 // second time from a cache.  It pays where there are lists for every compute unit (64
-// requests of up to 8000 tokens, 4 heads with 32 rows: dim 64 in bf16 51 us, by blocks
-// of 16 59; 128 in bf16 95 and 109; 192 in bf16 135 and 147) and not where the
-// blocks of 16 are more work to share out (8 requests of 4000, 20 rows of dim 128: 33 and
-// 24).  Not at all in fp32, dim 256, or fp16 of dim 128, where registers spill (as above:
-// 136 and 125 in fp32, 148 and 112 in fp16; dim 256 in bf16 234 and 226).
+// requests of up to 8000 tokens, 4 heads with 32 rows, bf16: dim 64 46 us, by blocks of 16
+// 49; 128 72 and 87; 192 118 and 119) and not where the blocks of 16 are more work to
+// share out (8 requests of 4000, 20 rows of dim 128: 35 and 25).  Not at all in fp32, dim
+// 256, or fp16 of dim 128, where registers spill (as above, dim 128: 257 and 96 in fp32, 97
+// and 87 in fp16; dim 256 in bf16 207 and 175).
 constexpr bool has_two(uint32_t type, uint32_t dim) { return type != UZIP_FP32 && dim <= 192 && !(type == UZIP_FP16 && dim == 128); }
-// Two workgroups to a compute unit where at most a few registers spill for it (32
-// requests, 20 rows of dim 128 in blocks of 32: 47 us, one to a unit 59; one row of dim
-// 192: 50 and 55; but of dim 256: 35 and 27).
+// Two workgroups to a compute unit where at most 6 registers spill for it (requests of 4000
+// tokens: 64, 20 rows of dim 128 in blocks of 32, 59 us, one to a unit 71; 32, 20 rows of
+// dim 192 48 and 62; but of dim 256 113 and 79).
 template <int T, int D, int NM>
 constexpr int kFewPerUnit = (D <= 128 || (D == 192 && NM == 1 && T != UZIP_FP32)) ? 2 : 1;
 template <int T, int CODE, int D, int NM>

@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
 // tokens that lie in one word of a value page's channel (values: the page is
 // transposed in registers); what it first loaded stays in registers until the exponent
 // is known.  Bound by the rows' bytes, each read from memory once: 16384 tokens of 8
-// heads of 128 in bf16, 101 MB in 20.8 us, 4.8 TB/s (value by value: 117 us).
+// heads of 128 in bf16, 101 MB in 20.9 us, 4.8 TB/s (value by value: 117 us).
 struct StoreArgs {
   Cache c;
   const void *x[2];
@@ -443,7 +443,7 @@ __device__ void store_run(const StoreArgs &a, uint32_t run, uint32_t h, uint32_t
 }
 
 // A run of one row by a wave: every lane a channel or a few, nothing but the row
-// number needed to ask for them.  64 rows of 8 heads: 4.3 us, by workgroups 5.0.
+// number needed to ask for them.  64 rows of 8 heads: 4.0 us, by workgroups 6.5.
 template <int T, int CODE>
 __device__ void store_one(const StoreArgs &a, bool values, int32_t row, uint32_t h, uint32_t lane) {
   typedef typename Elem<T>::type Value;
@@ -486,7 +486,7 @@ __global__ __launch_bounds__(256) void store_kernel(StoreArgs a) {
   if (blockIdx.z == 0) store_run<T, CODE, 256, false>(a, blockIdx.x, blockIdx.y, threadIdx.x, part, odd_part);
   else store_run<T, CODE, 256, true>(a, blockIdx.x, blockIdx.y, threadIdx.x, part, odd_part);
 }
-// Runs of a row or two: a wave for each.
+// A wave for each run, whatever its length.
 template <int T, int CODE>
 __global__ __launch_bounds__(256) void store_few_kernel(StoreArgs a) {
   const uint32_t h = blockIdx.y * 4 + (threadIdx.x >> 6);
@@ -499,7 +499,10 @@ __global__ __launch_bounds__(256) void store_few_kernel(StoreArgs a) {
 
 template <int T, int CODE>
 void launch_store(const StoreArgs &a, uint32_t max_runs, hipStream_t stream) {
-  // uzip_kv_max_runs allows a run for each row only where few rows share a page
+  // The host knows a bound on the runs, not their lengths.  A wave for each where the bound
+  // allows a run for every other row: steps of single tokens, but also a few long runs among
+  // many requests, which workgroups store faster (63 single rows and one run of 100: 12.5 us,
+  // 7.4), and plans made for more rows (8192 rows in pages of 16: 11.6 us, workgroups 20.6).
   if (a.n_rows <= 2 * max_runs) store_few_kernel<T, CODE><<<dim3(max_runs, (a.c.heads + 3) / 4, 2), 256, 0, stream>>>(a);
   else store_kernel<T, CODE><<<dim3(max_runs, a.c.heads, 2), 256, 0, stream>>>(a);
 }
