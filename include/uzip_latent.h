@@ -1,0 +1,97 @@
+/*
+ * uzip_latent.h -- latent attention on MI355X (gfx950): a paged 8-bit cache of one
+ * latent vector and one rotary key a token, its write, attention over it (absorbed
+ * form), and attention over a prompt's keys and values made from the latents
+ * (expanded form).
+ *
+ * With latent c_t, rotary key r_t and a head's matrices K, V:
+ *   expanded  s_t = scale (q . (K c_t) + p . r_t)      out = sum_t w_t (V c_t)
+ *   absorbed  s_t = scale ((K^T q) . c_t + p . r_t)    out = V (sum_t w_t c_t)
+ * with w = softmax(s).  The products with K, K^T and V are the caller's: they are
+ * linear layers.
+ *
+ * Cache layout (P = page_tokens, C = latent, R = rot):
+ *   codes u8 [n_pages][P][C + R]   a token's latent, then its rotary key
+ *   exps  u8 [n_pages][P][2]       exponent bytes of the two: code * 2^(e - 127)
+ * Scales are a token's own, so that a write never touches another token's codes.
+ *
+ * Conventions are those of uzip_kv.h; latent is 256 or 512, rot 32 or 64,
+ * page_tokens 16, 32, 64, 128 or 256, n_pages * page_tokens < 2^31.
+ */
+#ifndef UZIP_LATENT_H
+#define UZIP_LATENT_H
+
+#include "uzip_rotary.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef struct {
+  uint8_t *codes;
+  uint8_t *exps;
+  uint32_t n_pages;
+  uint32_t latent;
+  uint32_t rot;
+  uint32_t page_tokens;
+  uzip_dtype dtype;     /* UZIP_E4M3FN or UZIP_E5M2 */
+} uzip_latent_cache;
+
+/* Store new tokens: d_latent [n_rows][latent] and d_rot [n_rows][rot] at row strides (elements).
+ * The rotary key is turned (turn->rot is the cache's, first 0, inverse 0).  For each row and
+ * part: e is the least exponent byte in [27, 246] (e5m2: [27, 239]) with max |x| <= 448
+ * (57344) * 2^(e - 127) over the finite values; codes as uzip_kv_store makes them.
+ * d_slots as uzip_kv_plan makes them; rows whose slot is no place are not stored, and no
+ * two rows have the same slot.
+ * d_q [n_rows][n_q_heads][rot] (n_q_heads may be 0): the queries' rotary parts, turned into
+ * d_q_out in the same launch.
+ * Errors: EINVAL, EHIP, EUNSUPPORTED. */
+uzip_status uzip_latent_store(const uzip_latent_cache *cache, uzip_dtype dtype, const void *d_latent, int64_t latent_row,
+                              const void *d_rot, int64_t rot_row, uint32_t n_rows, const int64_t *d_slots,
+                              const uzip_turn *turn, const void *d_q, int64_t q_row, int64_t q_head, uint32_t n_q_heads,
+                              void *d_q_out, int64_t out_row, int64_t out_head, hipStream_t stream);
+
+/* Workspace of uzip_latent_attend in bytes; 0 for invalid arguments. */
+size_t uzip_latent_attend_workspace(uint32_t latent, uint32_t n_rows, uint32_t n_heads, uint32_t n_reqs,
+                                    uint32_t max_new);
+
+/* Absorbed form: each head's query [latent + rot] against the paged latents, which are
+ * keys and values of all heads.  Row j of request i stands at place p = d_lens[i] - n_i + j
+ * and sees the places 0 <= t <= p, as in uzip_kv_attend; out is [n_rows][n_heads][latent].
+ *   out = sum_t e^(s_t) c_t / sum_t e^(s_t)    lse = log sum_t e^(s_t)
+ * A row that sees nothing gives zeros and -infinity.  A token whose latent holds a NaN or an
+ * infinity makes the rows that see it NaN, and no others.
+ * dtype is UZIP_BF16 or UZIP_FP16.  Scores and sums are held in 32 bits; weights enter the second
+ * product with at least 8 bits for bf16, 12 for fp16.
+ *   max_new:  the most new tokens of a request: it chooses kernels, a wrong value costs
+ *             time and the last bits may differ.
+ * n_rows * n_heads <= UZIP_KV_MAX_ROW_HEADS; n_heads <= 1024; n_reqs <= UZIP_KV_MAX_REQUESTS.
+ * Errors: EINVAL, ENOSPC, EHIP, EUNSUPPORTED. */
+uzip_status uzip_latent_attend(const uzip_latent_cache *cache, uzip_dtype dtype, const void *d_q, int64_t q_row,
+                               int64_t q_head, uint32_t n_rows, uint32_t n_heads, const int32_t *d_table,
+                               uint32_t max_pages, const int32_t *d_lens, const int32_t *d_q_start, uint32_t n_reqs,
+                               uint32_t max_new, float scale, void *d_out, int64_t out_row, int64_t out_head,
+                               float *d_lse, void *d_ws, size_t ws_bytes, hipStream_t stream);
+
+/* Expanded form, for prompts: keys [n_keys][n_heads][nope], one rotary key [n_keys][rot] that all
+ * heads share, values [n_keys][n_heads][value]; a query is [nope + rot].  Request i's rows are
+ * d_q_start[i] .. d_q_start[i + 1], its keys d_k_start[i] .. d_k_start[i + 1]; row j of n_i
+ * stands at place (its keys) - n_i + j among them and sees the places up to its own.
+ * nope and value are 64 or 128, rot 32 or 64; dtype is UZIP_BF16 or UZIP_FP16.  Scores and sums are
+ * held in 32 bits; weights enter the second product in dtype.  A row that sees nothing gives zeros
+ * and -infinity.  A value that is infinite or NaN reaches the rows that see it, and no others.
+ *   max_new:  the most new tokens of a request: it chooses kernels, a wrong value costs time.
+ *   d_lse:    [n_rows][n_heads] (may be NULL).
+ * Errors: EINVAL, EHIP, EUNSUPPORTED. */
+uzip_status uzip_latent_attend_expanded(uzip_dtype dtype, const void *d_q, int64_t q_row, int64_t q_head, uint32_t n_rows,
+                                        uint32_t n_heads, const void *d_k, int64_t k_row, int64_t k_head,
+                                        const void *d_rot, int64_t rot_row, const void *d_v, int64_t v_row,
+                                        int64_t v_head, uint32_t n_keys, uint32_t nope, uint32_t rot, uint32_t value,
+                                        const int32_t *d_q_start, const int32_t *d_k_start, uint32_t n_reqs,
+                                        uint32_t max_new, float scale, void *d_out, int64_t out_row, int64_t out_head,
+                                        float *d_lse, hipStream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

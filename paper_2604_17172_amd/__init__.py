@@ -12,7 +12,11 @@ Convenience wrappers (``compress``, ``decompress``, ``reduce_fused``,
 the C ABI on ``torch.cuda.current_stream()``.
 
 The paged 8-bit key/value cache (``KVCache``, ``kv_plan``, ``kv_store``,
-``kv_attend``) is in ``kv.py``, its kernels in ``csrc/kv_*.hip``.
+``kv_attend``) is in ``kv.py``, its kernels in ``csrc/kv_*.hip``; rotary
+positions (``rotate``, ``kv_rotate_store``) are in ``rotary.py`` and
+``csrc/rotary.hip``, the latent cache (``LatentCache``, ``latent_store``,
+``latent_attend``, ``latent_attend_expanded``) in ``latent.py`` and
+``csrc/latent*.hip`` and ``csrc/expanded*.hip``.
 """
 from __future__ import annotations
 
@@ -442,3 +446,8 @@ def compress_chunked_table(x: torch.Tensor, block_bytes: int, chunk_bytes: int, 
 from .kv import (KV_MAX_REQUESTS, KV_MAX_ROWS, KVCache, KVPlan, kv_attend, kv_attend_workspace,  # noqa: E402,F401
                  kv_plan, kv_plan_buffers, kv_store, uzip_kv_attend, uzip_kv_attend_workspace, uzip_kv_cache,
                  uzip_kv_max_runs, uzip_kv_plan, uzip_kv_store)
+from .rotary import (kv_positions, kv_rotate_store, rotary_frequencies, rotate, uzip_kv_positions,  # noqa: E402,F401
+                     uzip_kv_rotate_store, uzip_rotate, uzip_turn)
+from .latent import (LatentCache, latent_attend, latent_attend_expanded, latent_attend_workspace, latent_store,  # noqa: E402,F401
+                     uzip_latent_attend, uzip_latent_attend_expanded, uzip_latent_attend_workspace, uzip_latent_cache,
+                     uzip_latent_store)

@@ -15,7 +15,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SRC = os.path.join(CSRC, "uzip.hip")
 SOURCES = [SRC] + [os.path.join(CSRC, name) for name in (
-    "kv_cache.hip", "kv_attend.hip", *(f"kv_attend_{dim}.hip" for dim in (64, 96, 128, 192, 256)))]
+    "kv_cache.hip", "kv_attend.hip", *(f"kv_attend_{dim}.hip" for dim in (64, 96, 128, 192, 256)),
+    "rotary.hip", "latent.hip", "latent_256.hip", "latent_512.hip",
+    "expanded.hip", "expanded_64.hip", "expanded_128.hip")]
 LIB_PATH = os.path.join(HERE, "_build", "libuzip.so")
 
 HIPCC_FLAGS = [
@@ -26,6 +28,11 @@ HIPCC_FLAGS = [
     "-ffp-contract=off",
     "-Wall", "-Wno-unused-command-line-argument",
 ]
+
+# Sources whose matrix instructions accumulate in vector registers: their sums are also rescaled, and
+# would move to the accumulation registers and back each time (a third of the loop's instructions).
+SOURCE_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+                for name in ("latent_256.hip", "latent_512.hip", "expanded_64.hip", "expanded_128.hip")}
 
 
 def _hipcc(args: list[str], verbose: bool) -> None:
@@ -44,7 +51,7 @@ def build(verbose: bool = False) -> str:
     try:
         units = [(src, os.path.join(objs, os.path.basename(src) + ".o")) for src in SOURCES]
         with ThreadPoolExecutor(max_workers=8) as pool:
-            for job in [pool.submit(_hipcc, ["-c", src, "-o", obj], verbose) for src, obj in units]:
+            for job in [pool.submit(_hipcc, [*SOURCE_FLAGS.get(os.path.basename(src), []), "-c", src, "-o", obj], verbose) for src, obj in units]:
                 job.result()
         tmp = LIB_PATH + ".tmp"
         _hipcc(["-shared", *[obj for _, obj in units], "-o", tmp], verbose)

@@ -1,0 +1,39 @@
+// latent_launch.h -- the launches of one width of latents; each latent_<width>.hip includes it
+// with LATENT_DIM, so that the widths compile side by side.
+#include <algorithm>
+
+#include "kv_host.h"
+#include "latent.h"
+#include "latent_host.h"
+
+namespace uzip_kv {
+
+template <int T, int CODE, int RG>
+static uzip_status launch(LatentCall &c) {
+  typedef Latent<T, CODE, LATENT_DIM, RG> L;
+  LatentArgs &a = c.a;
+  const auto kernel = latent_kernel<T, CODE, LATENT_DIM, RG>;
+  // At most how much work there is: blocks, and the tiles of each.
+  const uint64_t rows = (uint64_t)a.n_rows * a.heads, blocks = rows / L::kRows + a.n_reqs + 1;
+  const uint64_t tiles = ((uint64_t)a.max_pages << a.page_shift) / kTile + 2;
+  a.groups = (uint32_t)std::min<uint64_t>(c.units, std::max<uint64_t>(1, (std::min(blocks, rows) * tiles + L::kMin - 1) / L::kMin));
+  if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(typename L::Lds)) != hipSuccess) return UZIP_EHIP;
+  kernel<<<a.groups, L::kThreads, sizeof(typename L::Lds), c.stream>>>(a);
+  if (a.groups > 1)
+    latent_join_kernel<T, LATENT_DIM, L::kRows, L::kMin><<<dim3(a.groups - 1, L::kRows / 4), 256, 0, c.stream>>>(a);
+  return hipGetLastError() == hipSuccess ? UZIP_OK : UZIP_EHIP;
+}
+
+template <int T, int CODE>
+static uzip_status launch(LatentCall &c) {
+  return c.rows == 32 ? launch<T, CODE, 1>(c) : launch<T, CODE, 2>(c);
+}
+
+template <>
+uzip_status launch_latent<LATENT_DIM>(LatentCall &c) {
+  const bool e5 = c.code == UZIP_E5M2;
+  if (c.type == UZIP_BF16) return e5 ? launch<UZIP_BF16, UZIP_E5M2>(c) : launch<UZIP_BF16, UZIP_E4M3FN>(c);
+  return e5 ? launch<UZIP_FP16, UZIP_E5M2>(c) : launch<UZIP_FP16, UZIP_E4M3FN>(c);
+}
+
+}  // namespace uzip_kv

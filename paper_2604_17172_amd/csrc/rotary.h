@@ -1,0 +1,206 @@
+// rotary.h -- rotary positions: the turn of a head's pairs of channels.
+//
+// A row at position p turns pair i of its rotary part by the angle p f_i:
+//   a' = m (a cos - b sin)   b' = m (a sin + b cos)
+// with frequencies f and a magnitude m that the caller gives.  The matrix is m times
+// an orthogonal one, so the gradient is the same with the angle's sign changed.
+#pragma once
+
+#include "kv_host.h"
+#include "kv_store.h"
+#include "uzip_rotary.h"
+
+namespace uzip_kv {
+
+struct Turn {
+  const int32_t *positions;
+  const float *freq;   // [half]
+  uint32_t half;       // pairs
+  uint32_t first;      // channel where the rotary part begins
+  bool interleaved;    // pairs (2 i, 2 i + 1), else (i, i + half)
+  bool even;           // half and first are multiples of 8: no eight channels hold two kinds
+  float magnitude, sign;
+};
+
+struct CosSin {
+  float c, s;
+};
+
+// The angle is taken in 64 bits: at position 2^20 a product in 32 bits is off by up to 2^-4.
+// What is left of it after whole quarter turns goes to the two Taylor series up to
+// x^10, |x| <= pi / 4: the first term left out is below 2e-9.
+__device__ __forceinline__ CosSin turn_of(const Turn &t, int32_t p, uint32_t pair) {
+  const double quarters = (double)p * (double)t.freq[pair] * 0.63661977236758134308;  // 2 / pi
+  const double rest = quarters - 4.0 * __builtin_rint(0.25 * quarters);               // -2 .. 2
+  const double n = __builtin_rint(rest);
+  const float x = (float)((rest - n) * 1.57079632679489661923), z = x * x;
+  const int q = (int)n;
+  float s = __builtin_fmaf(z, 1.0f / 362880, -1.0f / 5040);
+  s = __builtin_fmaf(z, s, 1.0f / 120);
+  s = __builtin_fmaf(z, s, -1.0f / 6);
+  s = __builtin_fmaf(x * z, s, x);
+  float c = __builtin_fmaf(z, -1.0f / 3628800, 1.0f / 40320);
+  c = __builtin_fmaf(z, c, -1.0f / 720);
+  c = __builtin_fmaf(z, c, 1.0f / 24);
+  c = __builtin_fmaf(z, c, -0.5f);
+  c = __builtin_fmaf(z, c, 1.0f);
+  const float cc = q & 1 ? s : c, ss = q & 1 ? c : s;
+  // quarter turns: (c, s), (-s, c), (-c, -s), (s, -c)
+  const float m = t.magnitude;
+  return {((q + 1) & 2 ? -cc : cc) * m, (q & 2 ? -ss : ss) * m * t.sign};
+}
+
+__device__ __forceinline__ void turn_pair(const CosSin &r, float &a, float &b) {
+  const float x = a, y = b;
+  a = __builtin_fmaf(x, r.c, -(y * r.s));
+  b = __builtin_fmaf(x, r.s, y * r.c);
+}
+
+// The channels of a head, `dim` of them, in pairs: pair p < half is pair p of the rotary part,
+// the others are what lies before and after it, two by two.  `which` 0 or 1.
+__device__ __forceinline__ uint32_t channel_of(const Turn &t, uint32_t p, uint32_t which) {
+  if (p < t.half) return t.first + (t.interleaved ? 2 * p + which : p + which * t.half);
+  const uint32_t r = 2 * (p - t.half) + which;
+  return r < t.first ? r : r + 2 * t.half;
+}
+
+// A unit: pairs 8 u .. 8 u + 7.  With `even` its sixteen channels are two groups of eight; the
+// first channel of each.
+struct Groups {
+  uint32_t a, b;
+  bool turned;
+};
+__device__ __forceinline__ Groups groups_of(const Turn &t, uint32_t u) {
+  if (8 * u < t.half) {
+    const uint32_t a = t.first + (t.interleaved ? 16 * u : 8 * u);
+    return {a, t.interleaved ? a + 8 : a + t.half, true};
+  }
+  const uint32_t r = 16 * u - 2 * t.half;
+  return {r < t.first ? r : r + 2 * t.half, r + 8 < t.first ? r + 8 : r + 8 + 2 * t.half, false};
+}
+
+// Turns a unit's sixteen values (two groups of eight), rot(j) the turn of its pair j.
+template <class F>
+__device__ __forceinline__ void turn_unit(const Turn &t, float *x, const F &rot) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const CosSin r = rot(j);
+    if (t.interleaved) turn_pair(r, x[2 * j], x[2 * j + 1]);
+    else turn_pair(r, x[j], x[j + 8]);
+  }
+}
+
+// Division by a number known on the host, of n < 2^31.
+struct FastDiv {
+  uint32_t d, m, s;
+  static FastDiv of(uint32_t d) {
+    FastDiv f{d, 0, 0};
+    while ((1ull << f.s) < d) ++f.s;
+    f.m = (uint32_t)((((1ull << f.s) - d) << 32) / d + 1);
+    return f;
+  }
+  __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
+};
+
+// Rows of heads that are turned: [rows][heads][dim] at element strides.
+struct TurnRows {
+  const void *x;
+  void *out;
+  int64_t x_row, x_head, out_row, out_head;
+  uint32_t n_rows, heads, dim;
+  uint32_t block_rows;  // rows of a workgroup
+  uint32_t units;       // of a head, ceil(dim / 16)
+  FastDiv by_units, by_heads, by_half;
+  bool vec;             // rows start at multiples of 16 bytes, in whole groups of eight
+  bool in_place;        // out is x: what is not turned stays where it is
+};
+
+constexpr int kTurnThreads = 256;
+constexpr uint32_t kTurnTable = 1024;  // turns that a workgroup holds, at most: 8 KiB
+
+// One workgroup's rows.  The turns of a row are the same for all its heads: they are
+// worked out once, into LDS.
+template <int T>
+__device__ __forceinline__ void turn_rows(const TurnRows &a, const Turn &t, uint32_t block, CosSin *table) {
+  typedef typename Elem<T>::type Value;
+  const uint32_t r0 = block * a.block_rows, rows = min(a.block_rows, a.n_rows - r0), tid = threadIdx.x;
+  for (uint32_t i = tid; i < rows * t.half; i += kTurnThreads) {
+    const uint32_t r = a.by_half.div(i);
+    table[i] = turn_of(t, t.positions[r0 + r], i - r * t.half);
+  }
+  __syncthreads();
+  const uint32_t per_row = a.units * a.heads;
+  for (uint32_t i = tid; i < rows * per_row; i += kTurnThreads) {
+    const uint32_t rh = a.by_units.div(i), u = i - rh * a.units, r = a.by_heads.div(rh), h = rh - r * a.heads;
+    const Value *x = (const Value *)a.x + (int64_t)(r0 + r) * a.x_row + (int64_t)h * a.x_head;
+    Value *out = (Value *)a.out + (int64_t)(r0 + r) * a.out_row + (int64_t)h * a.out_head;
+    const CosSin *row = table + r * t.half;
+    if (a.vec) {
+      const Groups g = groups_of(t, u);
+      if (!g.turned && a.in_place) continue;
+      Eight<T> e[2];
+      e[0].load(x + g.a, true);
+      if (g.b < a.dim) e[1].load(x + g.b, true);
+      if (g.turned) {
+        float v[16];
+        e[0].get(v);
+        e[1].get(v + 8);
+        turn_unit(t, v, [&](int j) { return row[8 * u + j]; });
+        e[0].put(v);
+        e[1].put(v + 8);
+      }
+      e[0].store(out + g.a);
+      if (g.b < a.dim) e[1].store(out + g.b);
+    } else {
+#pragma unroll 1
+      for (uint32_t p = 8 * u; p < 8 * u + 8; ++p) {
+        const uint32_t ca = channel_of(t, p, 0), cb = channel_of(t, p, 1);
+        if (ca >= a.dim || (p >= t.half && a.in_place)) break;
+        if (p < t.half) {
+          float va = (float)x[ca], vb = (float)x[cb];
+          turn_pair(row[p], va, vb);
+          out[ca] = (Value)va;
+          out[cb] = (Value)vb;
+        } else {
+          const Value va = x[ca];
+          if (cb < a.dim) out[cb] = x[cb];
+          out[ca] = va;
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ host
+inline bool valid_turn(const uzip_turn *t) {
+  return t && t->rot >= 2 && t->rot <= 1024 && t->rot % 2 == 0 && t->first <= 1024 && t->interleaved <= 1 && t->inverse <= 1 &&
+         t->magnitude - t->magnitude == 0;
+}
+inline bool valid_places(const uzip_turn *t) { return t->positions && t->freq && aligned(t->positions, 4) && aligned(t->freq, 4); }
+
+inline Turn turn_args(const uzip_turn *t) {
+  const uint32_t half = t->rot / 2;
+  return {t->positions, t->freq, half, t->first, t->interleaved != 0, half % 8 == 0 && t->first % 8 == 0, t->magnitude, t->inverse ? -1.0f : 1.0f};
+}
+
+// What a launch over rows of heads needs; false where they cannot be.
+inline bool rows_to_turn(uzip_dtype dtype, const void *x, int64_t x_row, int64_t x_head, uint32_t n_rows, uint32_t heads, uint32_t dim,
+                         const uzip_turn *t, void *out, int64_t out_row, int64_t out_head, TurnRows *a) {
+  const uint32_t bytes = type_bytes(dtype);
+  if (heads == 0 || heads > 65535 || dim > 1024 || t->first + t->rot > dim || !valid_rows(x, x_row, x_head, bytes) ||
+      !valid_rows(out, out_row, out_head, bytes) || n_rows > UZIP_KV_MAX_ROWS || (uint64_t)n_rows * heads > UZIP_KV_MAX_ROW_HEADS)
+    return false;
+  auto whole = [&](const void *p, int64_t row, int64_t head) { return aligned(p, 16) && row * bytes % 16 == 0 && head * bytes % 16 == 0; };
+  const uint32_t half = t->rot / 2, units = (dim + 15) / 16, per_row = units * heads;
+  // Rows of a workgroup: four units to a thread, as long as there are rows for every compute unit and
+  // the table holds their turns.
+  uint32_t rows = 1;
+  while (rows * per_row < 4 * kTurnThreads && 2 * rows * half <= kTurnTable && n_rows > 512 * rows) rows *= 2;
+  *a = {x, out, x_row, x_head, out_row, out_head, n_rows, heads, dim, rows, units, FastDiv::of(units), FastDiv::of(heads), FastDiv::of(half),
+        half % 8 == 0 && t->first % 8 == 0 && dim % 8 == 0 && whole(x, x_row, x_head) && whole(out, out_row, out_head),
+        out == x && out_row == x_row && out_head == x_head};
+  return true;
+}
+inline uint32_t turn_blocks(const TurnRows &a) { return a.block_rows ? (a.n_rows + a.block_rows - 1) / a.block_rows : 0; }
+
+}  // namespace uzip_kv
