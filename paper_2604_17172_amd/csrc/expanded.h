@@ -145,6 +145,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 1 ? 2 : 1) void expanded_kernel
 
   // A kind of rows into LDS: `bytes` of a row, `row` bytes from one to the next in memory.
   auto stage = [&](auto width, const uint8_t *base, int64_t row, uint32_t t0, uint8_t *to) {
+    const uint32_t to_at = lds_at(to);
     constexpr int kBytes = decltype(width)::value, kChunks = kBytes / 16, kPer = 1024 / kBytes, kLoads = kTile / kPer;
     const uint32_t most = (uint32_t)b.keys - 1 - t0;
 #pragma unroll
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 1 ? 2 : 1) void expanded_kernel
       if (kLoads % WAVES && k >= kLoads) break;
       const uint32_t t = k * kPer + lane / kChunks, chunk = (lane % kChunks) ^ spread<kChunks>(t);
       if (a.direct) {
-        load_to_lds(base, min(t, most) * (uint32_t)row + chunk * 16, to + k * 1024);
+        load_to_lds(base, min(t, most) * (uint32_t)row + chunk * 16, to_at + k * 1024);
       } else {
         const Value *from = (const Value *)(base + (int64_t)min(t, most) * row) + chunk * 8;
         Value x[8] __attribute__((aligned(16)));
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 1 ? 2 : 1) void expanded_kernel
 #pragma unroll
         for (int e = 0; e < 16; ++e) most = fmaxf(most, s[n][e]);
       if (__any(most > m + kLag)) {
-        most = fmaxf(most, other_half(most));
+        most = max_of_halves(most);
         const float next = most > m + kLag ? most : m, f = next == m ? 1.0f : __builtin_amdgcn_exp2f(m - next);
         m = next;
         l *= f;
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 1 ? 2 : 1) void expanded_kernel
           acc[n] = mfma16(v.e, w[k], acc[n]);
         }
     }
-    l += other_half(l);
+    l = sum_of_halves(l);
     if (!careful) {  // a sum that is not finite is computed again with care
       float odd = l * 0.0f;
 #pragma unroll

@@ -13,6 +13,9 @@
 // out = acc / l, and the running maximum m is taken over g.
 #pragma once
 
+#include <type_traits>
+#include <utility>
+
 #include "kv_device.h"
 #include "uzip_latent.h"
 
@@ -37,6 +40,7 @@ struct LatentArgs {
   const int32_t *table, *lens, *q_start;
   float *part_acc;  // [slot][row][latent]
   float *part_ml;   // [slot][row][2]
+  struct LatentCut *cuts;  // of each workgroup
   uint32_t n_pages, page_shift, rot;
   uint32_t n_rows, heads, max_pages, n_reqs;
   uint32_t groups;    // workgroups that the work is shared by
@@ -45,6 +49,7 @@ struct LatentArgs {
 };
 
 constexpr int kTile = 64;  // tokens
+constexpr int kAhead = 4;  // reads of the first product under way
 
 // ------------------------------------------------------------------ pieces of work
 struct LatentRequest {
@@ -156,6 +161,27 @@ __device__ bool find_block(const LatentArgs &a, const F &x_of, Place *out) {
   return true;
 }
 
+// The same in all lanes, which the compiler is to know: it then holds it once for a wave.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x); }
+__device__ __forceinline__ void uniform(Place *p) {
+  uint32_t words[sizeof(Place) / 4];
+  __builtin_memcpy(words, p, sizeof(Place));
+#pragma unroll
+  for (uint32_t i = 0; i < sizeof(Place) / 4; ++i) words[i] = uniform(words[i]);
+  __builtin_memcpy(p, words, sizeof(Place));
+}
+
+// f(0), f(1), ... f(N - 1), the arguments constants: what f indexes with them stays in registers.
+template <int... I, class F>
+__device__ __forceinline__ void times(std::integer_sequence<int, I...>, const F &f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void times(const F &f) {
+  times(std::make_integer_sequence<int, N>{}, f);
+}
+
 // The block after p's, where there is one.
 template <int ROWS>
 __device__ __forceinline__ bool next_block(const LatentArgs &a, Place *p) {
@@ -225,6 +251,8 @@ struct LatentTile {
   float scale_c[kTile], scale_r[kTile];  // on the codes of the first product
   float mul[kTile];                      // fp16: on the scores
   float e[kTile], inv[kTile];            // e_t, 2^-e_t
+  uint64_t valid;                        // which tokens there are
+  uint8_t fill[248];                     // the next tile begins at a multiple of 256 bytes
 };
 __device__ __forceinline__ uint32_t swizzle(uint32_t t) { return ((t & 3) << 1) | ((t >> 2) & 1) | (t & 8); }
 
@@ -262,17 +290,34 @@ __device__ __forceinline__ typename LatentType<T>::Eight eight_codes(uint32_t lo
 __device__ __forceinline__ f32x16 mfma16(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma16(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
-
-// 16 bytes for each lane from base + offset on, into LDS side by side from `to` on.  Written out, so that the
-// compiler does not know of it: else it has every later read of LDS wait until all have arrived.  The
-// kernel waits itself, before the barrier that lets a tile be read.  (M0 holds where to; nothing else here uses it.)
-__device__ __forceinline__ void load_to_lds(const uint8_t *base, uint32_t offset, const void *to) {
-  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)to);
-  const uint32_t high = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32)), low = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
-  const uint64_t from = (uint64_t)high << 32 | low;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(offset), "s"(from) : "memory");
+// A lane's value and that of the lane 32 away, in one order for both.
+__device__ __forceinline__ f32x2 both_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
+__device__ __forceinline__ float max_of_halves(float x) {
+  const f32x2 r = both_halves(x);
+  return fmaxf(r[0], r[1]);
+}
+__device__ __forceinline__ float sum_of_halves(float x) {
+  const f32x2 r = both_halves(x);
+  return r[0] + r[1];
+}
+
+// 16 bytes for each lane from base + offset on, to LDS side by side from byte `to` of it on; base and `to` are the same
+// in all lanes.  Written out, so that the compiler does not know of it: else it has every later read of LDS
+// wait until all have arrived.  The kernel waits itself, before the barrier that lets a tile be read.  (M0
+// holds where to; nothing else here uses it.)
+__device__ __forceinline__ void load_to_lds(const uint8_t *base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(uniform(to)), "v"(offset), "s"(uniform((uint64_t)(uintptr_t)base)) : "memory");
+}
+// x, from which nothing is computed before this place: what only a seldom taken branch needs would else be
+// kept in registers through the loop around it.
+__device__ __forceinline__ uint32_t only_here(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ uint32_t lds_at(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 
 // Bytes of four codes that are NaN or infinite: their sign bits.
 template <int CODE>
@@ -280,260 +325,223 @@ __device__ __forceinline__ uint32_t not_numbers(uint32_t w) {
   return ((w & 0x7F7F7F7Fu) + (CODE == UZIP_E4M3FN ? 0x01010101u : 0x04040404u)) & 0x80808080u;
 }
 
-// RG groups of 32 rows, and two waves to each: in the first product each takes half of a tile's
-// tokens, in the second half of the channels, so that 32 x DC sums fit its registers
-// beside the queries.  A step of the loop is the scores of tile i, an exchange of their
-// maxima, and then its weights, beside which the matrix units take the second product of tile i - 1.
+// RG groups of 32 rows, and four waves to each.  Two score: each takes half of a tile's tokens, with the queries in
+// its registers, and makes their weights.  Two add: each takes half of the channels, with 32 x DC / 2 sums
+// in its registers, and asks for the tiles.  Scoring and adding a tile are a round apart, so that a compute unit's
+// matrix units have the products of the one beside the conversions and exponentials of the other; a wave that did both would
+// need all 512 registers, and nothing would run beside it (32 requests of 1000 to 16383 tokens, 128 heads: 126 us).
+// Between the two barriers of a round the scores' maxima are exchanged.
 template <int T, int CODE, int DC, int RG>
 struct Latent {
-  static constexpr int kRows = 32 * RG, kThreads = 128 * RG, kBlocks = DC / 64, kSteps = DC / 32, kBufs = 3;
-  static constexpr int kMin = 2;       // the least share of a workgroup
-  static constexpr float kLag = 3;     // weights up to 2^3: times 2^5 they are codes
+  static constexpr int kRows = 32 * RG, kThreads = 256 * RG, kBlocks = DC / 64, kSteps = DC / 32;
+  static constexpr int kBufs = 3;      // tiles in LDS: one whose values are read, one whose keys are, one under way
+  static constexpr int kMin = 4;       // the least share of a workgroup
+  static constexpr float kLag = 5;     // weights up to 2^5: times 2^3 they are codes
   typedef LatentTile<DC> Tile;
   struct Lds {
     Tile tile[kBufs];
-    i32x4 weights[RG][2][LatentType<T>::kTerms][64];  // of a wave's tokens, for the other
+    i32x4 weights[2][RG][2][LatentType<T>::kTerms][64];  // of two rounds: a half's tokens, as the lanes scored them
+    float factor[2][RG][32];                             // on the sums before them
     float most[RG][2][32];
-    float l[RG][2][32];
+    float m[RG][32], l[RG][2][32];
     uint32_t trouble;
     int32_t first_bad;
   };
+  static_assert(sizeof(Lds) <= 160 * 1024, "a compute unit's LDS");
 };
 
+// A block that several workgroups share, from `from` to `last`: noted by the first of them.
+struct LatentCut {
+  uint32_t cut;           // 0: this workgroup is not the first of one
+  int32_t first;          // row of the step's arrays of the request's first new token
+  uint32_t r0, rows;      // of the request's list
+  uint32_t from, last;
+};
+
+// The kernel's arguments, read once more: kept from its beginning to its end, those that only a block's beginning
+// or end needs would take the registers of the loop.
+__device__ __forceinline__ LatentArgs read_again() {
+  auto p = (const __attribute__((address_space(4))) LatentArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  LatentArgs a;
+  __builtin_memcpy(&a, (const LatentArgs *)p, sizeof(a));
+  return a;
+}
+
 template <int T, int CODE, int DC, int RG>
-__global__ __launch_bounds__(128 * RG, DC == 256 ? 2 : 1) void latent_kernel(LatentArgs a) {
+__global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
   typedef Latent<T, CODE, DC, RG> L;
   typedef typename Elem<T>::type Value;
   typedef typename LatentType<T>::Eight Eight;
   typedef typename L::Tile Tile;
-  constexpr int TERMS = LatentType<T>::kTerms, kWaves = 2 * RG;
+  typedef __attribute__((address_space(3))) i32x2 *LdsPair;
+  typedef const __attribute__((address_space(3))) u32x4 *LdsFour;
+  typedef const __attribute__((address_space(3))) f32x4 *LdsFloats;
+  typedef const __attribute__((address_space(3))) float *LdsFloat;
+  constexpr int TERMS = LatentType<T>::kTerms, kWaves = 2 * RG;  // of each kind
   extern __shared__ __align__(16) uint8_t lds_bytes[];
   typename L::Lds &lds = *(typename L::Lds *)lds_bytes;
-  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t rg = wave / 2, half = wave % 2, col = lane & 31, h = lane >> 5;
-
+  const uint32_t lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool adds = wave_of_all >= kWaves;
+  const uint32_t wave = wave_of_all % kWaves, rg = wave / 2, half = wave % 2, col = lane & 31, h = lane >> 5;
+  if (threadIdx.x == 0) args.cuts[blockIdx.x].cut = 0;
   uint64_t begin = 0, end = 0;
   Place place;
-  if (!find_block<L::kRows>(a, [&](uint64_t all, uint64_t *x) {
-        const uint64_t share = share_of<L::kMin>(a, all);
-        begin = share * blockIdx.x;
-        end = min(begin + share, all);
+  if (!find_block<L::kRows>(args, [&](uint64_t all, uint64_t *x) {
+        const uint64_t share = share_of<L::kMin>(args, all);
+        begin = uniform(share * blockIdx.x);
+        end = uniform((uint64_t)min(begin + share, all));
         *x = begin;
         return begin < all;
       }, &place))
     return;
 
   // what does not change from block to block
-  const uint32_t row_bytes = DC + a.rot, rot_steps = a.rot / 32;
-  // loads: 1 KiB at a time, 1024 / DC tokens of the latents, 16 of the rotary keys
+  const uint32_t lds0 = lds_at(lds_bytes), tiles0 = lds0 + (uint32_t)offsetof(typename L::Lds, tile);
+  const uint32_t row_bytes = DC + args.rot;
+  // Loads are of 1 KiB at a time, 1024 / DC tokens of the latents or 16 of the rotary keys.
   constexpr uint32_t kPer = 1024 / DC, kChunks = DC / 16, kLoads = kTile / kPer;
-  const uint32_t load_tok = lane / kChunks, rot_tok = lane / 4;
-  // the first product: token col of this wave's half, chunk 2 s + h
-  const uint32_t k_off = (32 * half + col) * DC + ((h ^ swizzle(col & 15)) << 4);
-  const uint32_t kr_off = (32 * half + col) * 64 + ((h ^ ((col >> 2) & 3)) << 4);
-  // the second: eight tokens by 16 channels for 16 lanes, from this wave's first channel on
-  const uint32_t j8 = (lane & 15) >> 1, v_tok = 8 * (j8 >> 2) + 4 * h + (j8 & 3);
-  const uint32_t channel0 = half * (DC / 2);
-  const uint32_t v_off = (v_tok * DC + ((((lane >> 4) & 1) ^ swizzle(v_tok)) << 4) + (lane & 1) * 8) ^ channel0;
+  // Tiles lie at multiples of 256 bytes, so that the exclusive or of an address's swizzle may come last.
+  static_assert(sizeof(Tile) % 256 == 0 && offsetof(typename L::Lds, tile) % 256 == 0 && offsetof(Tile, rot) % 256 == 0, "swizzled addresses");
 
   for (uint64_t x = begin; x < end;) {
+    const LatentArgs a = read_again();
+    uniform(&place);
     const uint64_t x1 = min(end, place.before + place.size);
     uint32_t tile0, tile1, tiles_all;
     tiles_of<L::kRows>(a, place, x, x1, &tile0, &tile1, &tiles_all);
+    tile0 = uniform(tile0);
+    tile1 = uniform(tile1);
     const LatentRequest &q = place.q;
-    const bool whole = tile0 == 0 && tile1 == tiles_all;
+    const bool whole = x == place.before && x1 == place.before + place.size;
     const uint32_t list = (uint32_t)q.rows * a.heads, r0 = place.block * L::kRows;
-    const uint32_t r = r0 + 32 * rg + col;
-    const bool here = r < list;
-    const uint32_t tok = here ? r / a.heads : 0, head = here ? r - tok * a.heads : 0;
-    const int32_t at = here ? q.base + (int32_t)tok : -1;       // the row's place
-    const uint32_t w0 = min(r0 + 32 * rg, list - 1);
-    const int32_t at_min = q.base + (int32_t)(w0 / a.heads);    // the first place of the wave's rows
-    const int32_t *table = a.table + (size_t)place.req * a.max_pages;
     const uint32_t rounds = tile1 - tile0;
+    if (!whole && x == place.before && threadIdx.x == 0)
+      a.cuts[blockIdx.x] = {1, q.first, r0, min(list - r0, (uint32_t)L::kRows), (uint32_t)blockIdx.x, (uint32_t)((place.before + place.size - 1) / (end - begin))};
 
-    if (rounds > 0 || whole) {
-      Eight query[2 * L::kSteps], query_rot[4];
-      {
-        const Value *src = (const Value *)a.q + (int64_t)(q.first + (int32_t)tok) * a.q_row + (int64_t)head * a.q_head;
-        auto get = [&](uint32_t d) {
-          Eight e;
-          if (!here) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = (Value)0.0f;
-          } else if (a.q_vec) {
-            e = *(const Eight *)(src + d);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = src[d + j];
-          }
-          return e;
-        };
-#pragma unroll
-        for (int s = 0; s < 2 * L::kSteps; ++s) query[s] = get(32 * (s / 2) + 16 * h + 8 * (s % 2));
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          if (s < 2 || rot_steps > 1) query_rot[s] = get(DC + 32 * (s / 2) + 16 * h + 8 * (s % 2));
-          else query_rot[s] = query_rot[0];
-        }
+    for (int careful = 0;; careful = 1) {
+      bool again;
+      if (threadIdx.x == 0) {
+        lds.trouble = 0;
+        lds.first_bad = INT32_MAX;
       }
-      for (int careful = 0;; careful = 1) {
-        f32x16 acc[L::kBlocks];
+      if (!adds) {
+        // ---------------------------------------------------------------- scores
+        const uint32_t r = r0 + 32 * rg + col;
+        const bool here = r < list;
+        const uint32_t tok = here ? r / a.heads : 0, head = here ? r - tok * a.heads : 0;
+        const int32_t at = here ? q.base + (int32_t)tok : -1;                                  // the row's place
+        const int32_t at_min = q.base + (int32_t)(min(r0 + 32 * rg, list - 1) / a.heads);      // the first of the wave's rows
+        const float scale_log2 = a.scale_log2;
+        Eight query[2 * L::kSteps + 4];
+        {
+          const Value *src = (const Value *)a.q + (int64_t)(q.first + (int32_t)tok) * a.q_row + (int64_t)head * a.q_head;
+          const bool vec = a.q_vec, two = a.rot > 32;
 #pragma unroll
-        for (int b = 0; b < L::kBlocks; ++b)
+          for (int s = 0; s < 2 * L::kSteps + 4; ++s) {
+            const uint32_t d = 32 * (s / 2) + 16 * h + 8 * (s % 2);
+            Eight e;
+            if (!here || (s >= 2 * L::kSteps + 2 && !two)) {  // of 32 rotary channels the keys' second half holds the first once more
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[b][i] = 0;
-        float m = -INFINITY, l = 0;
-        if (threadIdx.x == 0) {
-          lds.trouble = 0;
-          lds.first_bad = INT32_MAX;
-        }
-
-        auto page_of = [&](uint32_t tile) {  // of the tile's token `lane`; -1 for none
-          const int32_t t = (int32_t)(tile * kTile + lane);
-          int32_t p = -1;
-          if (tile < tile1 && t < q.len) p = table[(uint32_t)t >> a.page_shift];
-          return (uint32_t)p < a.n_pages ? p : -1;
-        };
-        uint64_t valid_next = 0;
-        uint32_t exps_next = 0;
-        // asks for a tile of whose tokens the lanes have the pages
-        auto ask = [&](uint32_t i, int32_t page) {
-          Tile *to = &lds.tile[i % L::kBufs];
-          valid_next = __ballot(page >= 0);
-          if (valid_next == 0) return;
-          const uint32_t safe = page < 0 ? 0 : (uint32_t)page, inside = (1u << a.page_shift) - 1;
-          const uint32_t slot = (safe << a.page_shift) + (((tile0 + i) * kTile + lane) & inside);
-#pragma unroll
-          for (uint32_t j = 0; j < kLoads / kWaves; ++j) {
-            const uint32_t k = j * kWaves + wave;  // this wave's
-            const uint32_t first = __builtin_amdgcn_readlane(slot, k * kPer);
-            const uint32_t chunk = (lane % kChunks) ^ swizzle((k * kPer + load_tok) & 15);
-            load_to_lds(a.codes + (size_t)first * row_bytes, load_tok * row_bytes + chunk * 16, to->latent + k * 1024);
-          }
-#pragma unroll
-          for (uint32_t j = 0; j < 4 / kWaves; ++j) {
-            const uint32_t k = j * kWaves + wave;
-            const uint32_t first = __builtin_amdgcn_readlane(slot, k * 16);
-            const uint32_t chunk = ((lane & 3) ^ ((rot_tok >> 2) & 3)) & (a.rot / 16 - 1);
-            load_to_lds(a.codes + (size_t)first * row_bytes, rot_tok * row_bytes + DC + chunk * 16, to->rot + k * 1024);
-          }
-          if (wave == 0) exps_next = *(const uint16_t *)(a.exps + 2 * (size_t)slot);
-        };
-        // waits for tile i, for all waves; what it needs beside the codes
-        auto arrive = [&](uint32_t i, uint64_t valid) {
-          Tile *tile = &lds.tile[i % L::kBufs];
-          __builtin_amdgcn_s_waitcnt(0);  // this wave's part has arrived
-          asm volatile("" ::: "memory");
-          if (wave == 0) {
-            const bool ok = valid >> lane & 1;
-            const uint32_t ec = ok ? max(exps_next & 0xFF, 1u) : 127, er = ok ? max(exps_next >> 8 & 0xFF, 1u) : 127;
-            if constexpr (T == UZIP_FP16) {  // fp16 holds codes times powers of two up to 1
-              const uint32_t most = max(ec, er);
-              tile->scale_c[lane] = pow2(max(127 + (int)ec - (int)most, 1));
-              tile->scale_r[lane] = pow2(max(127 + (int)er - (int)most, 1));
-              tile->mul[lane] = a.scale_log2 * pow2(most);
+              for (int j = 0; j < 8; ++j) e[j] = (Value)0.0f;
+            } else if (vec) {
+              e = *(const Eight *)(src + d);
             } else {
-              tile->scale_c[lane] = pow2(ec);
-              tile->scale_r[lane] = pow2(er);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) e[j] = src[d + j];
             }
-            tile->e[lane] = (float)((int)ec - 127);
-            tile->inv[lane] = pow2(254 - (int)ec);
+            query[s] = e;
           }
-          if (~valid) {  // codes of places that are none count as zero
-#pragma unroll 1
-            for (uint32_t k = wave; k < kLoads; k += kWaves)
-              if (!(valid >> (k * kPer + load_tok) & 1)) *(u32x4 *)(tile->latent + k * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-#pragma unroll 1
-            for (uint32_t k = wave; k < 4; k += kWaves)
-              if (!(valid >> (k * 16 + rot_tok) & 1)) *(u32x4 *)(tile->rot + k * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-          }
-          __syncthreads();
-          if (careful) {  // tokens that hold a NaN or an infinity are left out and noted
-#pragma unroll 1
-            for (uint32_t k = wave; k < kLoads; k += kWaves) {
-              u32x4 *c = (u32x4 *)(tile->latent + k * 1024 + lane * 16);
-              const bool bad = (not_numbers<CODE>(c->x) | not_numbers<CODE>(c->y) | not_numbers<CODE>(c->z) | not_numbers<CODE>(c->w)) != 0;
-              const uint64_t bads = __ballot(bad) >> (load_tok * kChunks) & ((1ull << kChunks) - 1);
-              if (bads) {
-                *c = u32x4{0, 0, 0, 0};
-                if (lane % kChunks == 0) atomicMin(&lds.first_bad, (int32_t)((tile0 + i) * kTile + k * kPer + load_tok));
-              }
-            }
-            __syncthreads();
-          }
-        };
-        // scores of this wave's 32 tokens of tile i, times log2(e), plus e_t; their largest
-        auto score = [&](uint32_t i, uint64_t valid, f32x16 &s) {
-          const Tile *tile = &lds.tile[i % L::kBufs];
-          const int32_t t0 = (int32_t)((tile0 + i) * kTile);
-          const float sc = tile->scale_c[32 * half + col], sr = tile->scale_r[32 * half + col];
-          f32x16 s1;
+        }
+        // token col of this wave's half, chunk 2 k + h
+        const uint32_t k_off = (32 * half + col) * DC + ((h ^ swizzle(col & 15)) << 4);
+        const uint32_t r_off = (uint32_t)offsetof(Tile, rot) + (32 * half + col) * 64 + ((h ^ ((col >> 2) & 3)) << 4);
+        float m = -INFINITY, l = 0;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[e] = s1[e] = 0;
+        for (int term = 0; term < TERMS; ++term) lds.weights[1][rg][half][term][lane] = i32x4{0, 0, 0, 0};  // before the first
+        lds.factor[1][rg][col] = 1;
+        for (uint32_t i = 0; i < rounds; ++i) {
+          __syncthreads();  // tile i is there
+          if (careful) __syncthreads();
+          const uint32_t tile = tiles0 + i % L::kBufs * (uint32_t)sizeof(Tile);
+          const uint32_t of_token = tile + 4 * (32 * half + col), of_four = tile + 4 * (32 * half + 4 * h);
+          const float sc = *(LdsFloat)(uintptr_t)(of_token + offsetof(Tile, scale_c)), sr = *(LdsFloat)(uintptr_t)(of_token + offsetof(Tile, scale_r));
+          const uint32_t k_at = tile + k_off, r_at = tile + r_off;
+          // The order is written down, between barriers to the compiler's scheduler: reads some steps ahead.
+          constexpr int kReads = L::kSteps + 2;
+          auto chunk = [&](int k) {
+            return k < L::kSteps ? *(LdsFour)(uintptr_t)((k_at ^ ((k & 7) << 5)) + (k >> 3) * 256) : *(LdsFour)(uintptr_t)(r_at ^ ((k - L::kSteps) << 5));
+          };
+          f32x16 s;
 #pragma unroll
-          for (int k = 0; k < L::kSteps; ++k) {
-            const u32x4 c = *(const u32x4 *)(tile->latent + (k_off ^ ((k & 7) << 5)) + (k >> 3) * 256);
-            s = mfma16(eight_codes<CODE, T>(c.x, c.y, sc), query[2 * k], s);
-            s1 = mfma16(eight_codes<CODE, T>(c.z, c.w, sc), query[2 * k + 1], s1);
-          }
+          for (int e = 0; e < 16; ++e) s[e] = 0;
+          u32x4 c[kAhead];
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            if (k && rot_steps < 2) break;
-            const u32x4 c = *(const u32x4 *)(tile->rot + (kr_off ^ (k << 5)));
-            s = mfma16(eight_codes<CODE, T>(c.x, c.y, sr), query_rot[2 * k], s);
-            s1 = mfma16(eight_codes<CODE, T>(c.z, c.w, sr), query_rot[2 * k + 1], s1);
-          }
+          for (int k = 0; k < kAhead; ++k) c[k] = chunk(k);
+          __builtin_amdgcn_sched_barrier(0);
+          times<kReads>([&](auto number) {
+            constexpr int k = decltype(number)::value;
+            const u32x4 now = c[k % kAhead];
+            if constexpr (k + kAhead < kReads) c[k % kAhead] = chunk(k + kAhead);
+            const float scale = k < L::kSteps ? sc : sr;
+            s = mfma16(eight_codes<CODE, T>(now.x, now.y, scale), query[2 * k], s);
+            s = mfma16(eight_codes<CODE, T>(now.z, now.w, scale), query[2 * k + 1], s);
+            __builtin_amdgcn_sched_barrier(0);
+          });
+          // times log2(e), plus e_t; the largest
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const f32x4 e = *(const f32x4 *)(tile->e + 32 * half + 8 * g + 4 * h);
+            const f32x4 e = *(LdsFloats)(uintptr_t)(of_four + offsetof(Tile, e) + 32 * g);
             f32x4 mul;
-            if constexpr (T == UZIP_FP16) mul = *(const f32x4 *)(tile->mul + 32 * half + 8 * g + 4 * h);
+            if constexpr (T == UZIP_FP16) mul = *(LdsFloats)(uintptr_t)(of_four + offsetof(Tile, mul) + 32 * g);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[4 * g + k] = __builtin_fmaf(s[4 * g + k] + s1[4 * g + k], T == UZIP_FP16 ? mul[k] : a.scale_log2, e[k]);
+            for (int k = 0; k < 4; ++k) s[4 * g + k] = __builtin_fmaf(s[4 * g + k], T == UZIP_FP16 ? mul[k] : scale_log2, e[k]);
           }
+          const int32_t t0 = (int32_t)((tile0 + i) * kTile);
+          const uint64_t valid = lds.tile[i % L::kBufs].valid;
           if (~valid || t0 + kTile - 1 > at_min) {
-            const uint32_t mine = (uint32_t)(valid >> (32 * half + 4 * h));
+            const uint32_t there = (uint32_t)(valid >> (32 * half + 4 * h));
             const int32_t upto = at - t0 - 32 * (int)half - 4 * (int)h;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const int k = 8 * (e / 4) + e % 4;
-              s[e] = (mine >> k & 1) && k <= upto ? s[e] : -INFINITY;
+              s[e] = (there >> k & 1) && k <= upto ? s[e] : -INFINITY;
             }
           }
           float most = -INFINITY;
 #pragma unroll
           for (int e = 0; e < 16; ++e) most = fmaxf(most, s[e]);
-          most = fmaxf(most, other_half(most));
+          most = max_of_halves(most);
           if (h == 0) lds.most[rg][half][col] = most;
-        };
-        // The maxima of both halves are there: the weights, in this wave's registers and for the
-        // other; the factor on the sums so far.
-        auto weigh = [&](uint32_t i, const f32x16 &s, i32x4 *w) {
-          const Tile *tile = &lds.tile[i % L::kBufs];
-          const float most = fmaxf(lds.most[rg][0][col], lds.most[rg][1][col]);
+          __syncthreads();
+
+          // the reference of this tile's weights, the factor on the sums so far, the weights
+          f32x4 inv[4];
+#pragma unroll
+          for (int g = 0; g < 4; ++g) inv[g] = *(LdsFloats)(uintptr_t)(of_four + offsetof(Tile, inv) + 32 * g);
+          most = fmaxf(lds.most[rg][0][col], lds.most[rg][1][col]);
           const float next = most > m + L::kLag ? most : m;
           const float f = next == m ? 1.0f : __builtin_amdgcn_exp2f(m - next);
           m = next;
           l *= f;
-          const float ref = m == -INFINITY ? 0.0f : m;
+          if (half == 0 && h == 0) lds.factor[i & 1][rg][col] = f;
+          const float ref = m == -INFINITY ? 0.0f : m - 3.0f;
+          i32x4 w[TERMS];
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const f32x4 inv = *(const f32x4 *)(tile->inv + 32 * half + 8 * g + 4 * h);
             float y[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              y[k] = __builtin_amdgcn_exp2f(s[4 * g + k] - ref);
-              l = __builtin_fmaf(y[k], inv[k], l);
-              y[k] *= 32.0f;
+              y[k] = __builtin_amdgcn_exp2f(s[4 * g + k] - ref);  // 2^3 times the weight
+              l = __builtin_fmaf(y[k], inv[g][k], l);
             }
 #pragma unroll
             for (int term = 0; term < TERMS; ++term) {
-              int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-              c = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
-              w[term][g] = c;
+              int code = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+              code = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], code, true);
+              w[term][g] = code;
               if (term + 1 < TERMS) {
-                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(code, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(code, true);
                 y[0] = (y[0] - lo[0]) * 16.0f;
                 y[1] = (y[1] - lo[1]) * 16.0f;
                 y[2] = (y[2] - hi[0]) * 16.0f;
@@ -541,103 +549,204 @@ __global__ __launch_bounds__(128 * RG, DC == 256 ? 2 : 1) void latent_kernel(Lat
               }
             }
           }
-          return f;
-        };
-        auto pass_on = [&](const i32x4 *w) {
 #pragma unroll
-          for (int term = 0; term < TERMS; ++term) lds.weights[rg][half][term][lane] = w[term];
-        };
-        auto take_over = [&](i32x4 *w) {
+          for (int term = 0; term < TERMS; ++term) lds.weights[i & 1][rg][half][term][lane] = w[term];
+        }
+        // the adding waves' last round
+        __syncthreads();
+        l = sum_of_halves(l);
+        if (h == 0) {
+          lds.l[rg][half][col] = l;
+          lds.m[rg][col] = m - 3.0f;  // what the weights' sums count from
+        }
+        if (__any(l * 0.0f != 0.0f) && lane == 0) lds.trouble = 1;
+        __syncthreads();
+        again = !careful && lds.trouble != 0;
+        __syncthreads();
+      } else {
+        // ---------------------------------------------------------------- sums
+        f32x16 acc[L::kBlocks];
 #pragma unroll
-          for (int term = 0; term < TERMS; ++term) w[term] = lds.weights[rg][1 - half][term][lane];
-        };
-        // sums of tile i's latents with the weights of this wave's tokens and the other's
-        auto add_up = [&](uint32_t i, const i32x4 *mine, const i32x4 *others) {
-          const uint8_t *v = lds.tile[i % L::kBufs].latent;
-          constexpr int kKind = CODE == UZIP_E4M3FN ? 0 : 1;
-          i32x8 w[TERMS];
+        for (int b = 0; b < L::kBlocks; ++b)
 #pragma unroll
-          for (int term = 0; term < TERMS; ++term)
+          for (int e = 0; e < 16; ++e) acc[b][e] = 0;
+        const uint32_t channel0 = half * (DC / 2);
+        // eight tokens by 16 channels for 16 lanes, from this wave's first channel on
+        const uint32_t j8 = (lane & 15) >> 1, v_tok = 8 * (j8 >> 2) + 4 * h + (j8 & 3);
+        const uint32_t v_off = (v_tok * DC + ((((lane >> 4) & 1) ^ swizzle(v_tok)) << 4) + (lane & 1) * 8) ^ channel0;
+        // Where a lane's part of load k = j kWaves + wave lies from its 16 tokens' first code on: the same for every kPeriod-th j, for
+        // swizzle() of a sum without carries is the exclusive or of its parts'.
+        constexpr int kWaveTokens = kWaves * kPer, kPeriod = 16 / kWaveTokens;
+        static_assert(16 % kWaveTokens == 0, "a round of loads lies in one page");
+        uint32_t load_off[kPeriod];
+#pragma unroll
+        for (int j = 0; j < kPeriod; ++j) {
+          const uint32_t t = j * kWaveTokens + wave * kPer + lane / kChunks;
+          load_off[j] = t * row_bytes + (((lane % kChunks) ^ swizzle(t)) << 4);
+        }
+        const uint32_t rot_off = lane / 4 * row_bytes + DC + ((((lane & 3) ^ ((lane >> 4) & 3)) & (a.rot / 16 - 1)) << 4);
+        const int32_t *table = a.table + (size_t)place.req * a.max_pages;
+
+        auto page_of = [&](uint32_t i) {  // of tile i's token `lane`; -1 for none
+          const int32_t t = (int32_t)((tile0 + i) * kTile + lane);
+          int32_t p = -1;
+          if (i < rounds && t < q.len) p = table[(uint32_t)t >> a.page_shift];
+          return (uint32_t)p < a.n_pages ? p : -1;
+        };
+        // What the loads of a tile go by: where its tokens' codes lie, one to a lane, and which of them there are.
+        struct Next {
+          uint64_t at, valid;
+          uint32_t exps;
+        };
+        auto next_of = [&](uint32_t i, int32_t page) {  // codes of some page where there is none
+          const uint32_t slot = ((page < 0 ? 0 : (uint32_t)page) << a.page_shift) + (((tile0 + i) * kTile + lane) & ((1u << a.page_shift) - 1));
+          return Next{(uint64_t)(uintptr_t)a.codes + (uint64_t)slot * row_bytes, (uint64_t)__ballot(page >= 0),
+                      wave == 0 ? (uint32_t) * (const uint16_t *)(a.exps + 2 * (size_t)slot) : 0u};
+        };
+        // this wave's loads of tile i
+        constexpr int kCodes = kLoads / kWaves;
+        auto ask = [&](uint32_t i, const Next &n) {
+          auto from = [&](uint32_t token) {
+            const uint32_t low = __builtin_amdgcn_readlane((uint32_t)n.at, token), high = __builtin_amdgcn_readlane((uint32_t)(n.at >> 32), token);
+            return (const uint8_t *)(uintptr_t)((uint64_t)high << 32 | low);
+          };
+          const uint32_t to = tiles0 + i % L::kBufs * (uint32_t)sizeof(Tile) + wave * 1024;
+          times<kCodes>([&](auto number) {
+            constexpr int j = decltype(number)::value;
+            load_to_lds(from(j * kWaveTokens / 16 * 16), load_off[j % kPeriod], to + (uint32_t)offsetof(Tile, latent) + j * kWaves * 1024);
+          });
+          times<4 / kWaves>([&](auto number) {
+            constexpr int j = decltype(number)::value;
+            load_to_lds(from(16 * (j * kWaves + wave)), rot_off, to + (uint32_t)offsetof(Tile, rot) + j * kWaves * 1024);
+          });
+        };
+        // what a tile needs beside the codes, from its tokens' exponents
+        auto scales = [&](uint32_t i, const Next &n) {
+          if (wave != 0) return;
+          const uint32_t lane = only_here(threadIdx.x & 63);
+          Tile *tile = &lds.tile[i % L::kBufs];
+          const bool ok = n.valid >> lane & 1;
+          const uint32_t ec = ok ? max(n.exps & 0xFF, 1u) : 127, er = ok ? max(n.exps >> 8 & 0xFF, 1u) : 127;
+          if constexpr (T == UZIP_FP16) {  // fp16 holds codes times powers of two up to 1
+            const uint32_t most = max(ec, er);
+            tile->scale_c[lane] = pow2(max(127 + (int)ec - (int)most, 1));
+            tile->scale_r[lane] = pow2(max(127 + (int)er - (int)most, 1));
+            tile->mul[lane] = a.scale_log2 * pow2(most);
+          } else {
+            tile->scale_c[lane] = pow2(ec);
+            tile->scale_r[lane] = pow2(er);
+          }
+          tile->e[lane] = (float)((int)ec - 127);
+          tile->inv[lane] = pow2(254 - (int)ec);
+          if (lane == 0) tile->valid = n.valid;
+        };
+
+        Next then{};  // of tile i + 1
+        int32_t page_after = -1;
+        uint64_t now_valid = 0;
+        if (rounds > 0) {
+          const Next now = next_of(0, page_of(0));
+          now_valid = now.valid;
+          ask(0, now);
+          then = next_of(1, page_of(1));
+          page_after = page_of(2);
+          scales(0, now);
+        }
+        uint64_t valid = now_valid;
+        for (uint32_t i = 0; i <= rounds; ++i) {
+          __builtin_amdgcn_s_waitcnt(0);  // this wave's part of tile i has arrived
+          asm volatile("" ::: "memory");
+          if (~valid && i < rounds) {  // codes of places that are none count as zero
+            Tile *tile = &lds.tile[i % L::kBufs];
+            const uint32_t lane = only_here(threadIdx.x & 63), tok = lane / kChunks;
+#pragma unroll 1
+            for (uint32_t k = wave; k < kLoads; k += kWaves)
+              if (!(valid >> (k * kPer + tok) & 1)) *(u32x4 *)(tile->latent + k * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+#pragma unroll 1
+            for (uint32_t k = wave; k < 4; k += kWaves)
+              if (!(valid >> (k * 16 + lane / 4) & 1)) *(u32x4 *)(tile->rot + k * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+          }
+          __syncthreads();
+          if (careful && i < rounds) {  // tokens that hold a NaN or an infinity are left out and noted
+            Tile *tile = &lds.tile[i % L::kBufs];
+            const uint32_t lane = only_here(threadIdx.x & 63), tok = lane / kChunks;
+#pragma unroll 1
+            for (uint32_t k = wave; k < kLoads; k += kWaves) {
+              u32x4 *c = (u32x4 *)(tile->latent + k * 1024 + lane * 16);
+              const bool bad = (not_numbers<CODE>(c->x) | not_numbers<CODE>(c->y) | not_numbers<CODE>(c->z) | not_numbers<CODE>(c->w)) != 0;
+              const uint64_t bads = __ballot(bad) >> (tok * kChunks) & ((1ull << kChunks) - 1);
+              if (bads) {
+                *c = u32x4{0, 0, 0, 0};
+                if (lane % kChunks == 0) atomicMin(&lds.first_bad, (int32_t)((tile0 + i) * kTile + k * kPer + tok));
+              }
+            }
+            __syncthreads();
+          }
+          if (rounds == 0) break;
+          if (i + 1 < rounds) {
+            ask(i + 1, then);
+            scales(i + 1, then);
+          }
+          valid = then.valid;
+          then = next_of(i + 2, page_after);
+          page_after = page_of(i + 3);
+
+          // The products of tile i - 1; in the first round of tile 0 and weights that are 0.
+          const uint32_t before = tiles0 + (i ? i - 1 : 0) % L::kBufs * (uint32_t)sizeof(Tile) + v_off;
+          const float f = lds.factor[(i + 1) & 1][rg][col];
+          i32x8 w[TERMS], v[2];
+#pragma unroll
+          for (int term = 0; term < TERMS; ++term) {
+            const i32x4 first = lds.weights[(i + 1) & 1][rg][0][term][lane], second = lds.weights[(i + 1) & 1][rg][1][term][lane];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-              w[term][g] = half ? others[term][g] : mine[term][g];
-              w[term][4 + g] = half ? mine[term][g] : others[term][g];
+              w[term][g] = first[g];
+              w[term][4 + g] = second[g];
             }
+          }
+          if (__any(f != 1.0f)) {
 #pragma unroll
-          for (int b = 0; b < L::kBlocks; ++b) {
-            i32x8 c;
+            for (int b = 0; b < L::kBlocks; ++b)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) acc[b][e] *= f;
+          }
+          auto values = [&](int b) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const i32x2 p = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                  (__attribute__((address_space(3))) i32x2 *)(v + (v_off ^ ((b & 7) << 5)) + (b >> 3) * 256 + k * 16 * DC));
-              c[2 * k] = p[0];
-              c[2 * k + 1] = p[1];
+              const i32x2 p = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LdsPair)(uintptr_t)((before ^ ((b & 7) << 5)) + (b >> 3) * 256 + k * 16 * DC));
+              v[b % 2][2 * k] = p[0];
+              v[b % 2][2 * k + 1] = p[1];
             }
+          };
+          values(0);
+#pragma unroll
+          for (int b = 0; b < L::kBlocks; ++b) {
+            if (b + 1 < L::kBlocks) values(b + 1);
 #pragma unroll
             for (int term = 0; term < TERMS; ++term)
-              acc[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(c, w[term], acc[b], kKind, 0, 0, 127, 0, 122 - 4 * term);
+              acc[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v[b % 2], w[term], acc[b], CODE == UZIP_E4M3FN ? 0 : 1, 0, 0, 127, 0, 127 - 4 * term);
+            if (b == L::kBlocks / 2 - 1 && i < rounds) __syncthreads();
           }
-        };
-
-        if (rounds > 0) {
-          i32x4 mine[TERMS], others[TERMS];
-          ask(0, page_of(tile0));
-          int32_t page_next = page_of(tile0 + 1);
-          uint64_t valid = valid_next;
-          arrive(0, valid);
-          ask(1, page_next);
-          page_next = page_of(tile0 + 2);
-          f32x16 s;
-          score(0, valid, s);
-          __syncthreads();
-          weigh(0, s, mine);
-          pass_on(mine);
-          for (uint32_t i = 1; i < rounds; ++i) {
-            valid = valid_next;
-            arrive(i, valid);
-            ask(i + 1, page_next);
-            page_next = page_of(tile0 + i + 2);
-            take_over(others);
-            score(i, valid, s);
-            __syncthreads();
-            i32x4 next[TERMS];
-            const float f = weigh(i, s, next);
-            add_up(i - 1, mine, others);
-            if (__any(f != 1.0f)) {
-#pragma unroll
-              for (int b = 0; b < L::kBlocks; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[b][e] *= f;
-            }
-            pass_on(next);
-#pragma unroll
-            for (int term = 0; term < TERMS; ++term) mine[term] = next[term];
-          }
-          __syncthreads();
-          take_over(others);
-          add_up(rounds - 1, mine, others);
         }
-
-        // the sums of a row's tokens from the halves of two waves
-        l += other_half(l);
-        if (h == 0) lds.l[rg][half][col] = l;
-        float odd = l * 0.0f;
-        if (!careful) {  // a sum that is not finite is computed again with care
+        // a sum that is not finite is computed again with care
+        float odd = 0;
+        if (!careful) {
 #pragma unroll
           for (int b = 0; b < L::kBlocks; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) odd = __builtin_fmaf(acc[b][e], 0.0f, odd);
-          if (rounds == 0) __syncthreads();  // the mark is set after it was cleared
-          if (__any(odd != 0.0f) && lane == 0) lds.trouble = 1;
         }
+        if (__any(odd != 0.0f) && lane == 0) lds.trouble = 1;
         __syncthreads();
-        l = lds.l[rg][0][col] + lds.l[rg][1][col];
-        const bool again = !careful && lds.trouble != 0;
-        if (careful && at >= lds.first_bad) l = NAN;
+        again = !careful && lds.trouble != 0;
+        const uint32_t col = only_here(threadIdx.x & 31), h = only_here(threadIdx.x & 63) >> 5, r = r0 + 32 * rg + col;
+        const uint32_t tok = r / a.heads, head = r - tok * a.heads;
+        float l = lds.l[rg][0][col] + lds.l[rg][1][col];
+        const float m = lds.m[rg][col];
+        if (careful && q.base + (int32_t)tok >= lds.first_bad) l = NAN;
         __syncthreads();
-        if (again) continue;
-
-        if (here) {
+        if (!again && r < list) {
+          const LatentArgs a = read_again();
           if (whole) {
             const float f = l > 0 ? 1.0f / l : l == 0 ? 0.0f : NAN;
             Value *out = (Value *)a.out + (int64_t)(q.first + (int32_t)tok) * a.out_row + (int64_t)head * a.out_head + channel0;
@@ -661,7 +770,7 @@ __global__ __launch_bounds__(128 * RG, DC == 256 ? 2 : 1) void latent_kernel(Lat
           } else {
             const size_t slot = 2 * (size_t)blockIdx.x + (begin > place.before ? 0 : 1), row = slot * L::kRows + 32 * rg + col;
 #pragma unroll
-            for (int b = 0; b < L::kBlocks; ++b)
+            for (int b = 0; b < L::kBlocks && rounds > 0; ++b)
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
                 f32x4 y;
@@ -675,61 +784,64 @@ __global__ __launch_bounds__(128 * RG, DC == 256 ? 2 : 1) void latent_kernel(Lat
             }
           }
         }
-        break;
       }
+      if (!again) break;
     }
     x = x1;
-    if (x < end && !next_block<L::kRows>(a, &place)) break;
+    if (x < end && !next_block<L::kRows>(read_again(), &place)) break;
   }
 }
 
-// The pieces of a block that several workgroups shared, one wave a row.  Workgroup (w, y): the block that
-// the boundary between workgroups w and w + 1 cuts, if it is the first to cut it.
-template <int T, int DC, int ROWS, int MIN>
+// The pieces of a block that several workgroups shared.  Workgroup (w, y): four rows, a wave each, of the block that workgroup w
+// was the first of.
+template <int T, int DC, int ROWS>
 __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
   typedef typename Elem<T>::type Value;
-  uint64_t share = 0, x = 0, all_work = 0;
-  Place p;
-  if (!find_block<ROWS>(a, [&](uint64_t all, uint64_t *at) {
-        share = share_of<MIN>(a, all);
-        all_work = all;
-        x = *at = share * (blockIdx.x + 1);
-        return x < all;
-      }, &p))
-    return;
-  if (p.before >= x || p.before < x - share) return;  // not cut there, or also before
-  const uint32_t lane = threadIdx.x & 63, list = (uint32_t)p.q.rows * a.heads;
-  const uint32_t i = blockIdx.y * 4 + (threadIdx.x >> 6), r = p.block * ROWS + i;
-  if (r >= list) return;
-  const uint32_t tok = r / a.heads, head = r - tok * a.heads;
-  const uint32_t from = blockIdx.x, last = (uint32_t)((p.before + p.size - 1) / share);
+  const LatentCut c = a.cuts[blockIdx.x];
+  const uint32_t lane = threadIdx.x & 63, i = blockIdx.y * 4 + (threadIdx.x >> 6);
+  if (!c.cut || i >= c.rows) return;
+  const uint32_t r = c.r0 + i, tok = r / a.heads, head = r - tok * a.heads;
+  // the piece of workgroup w: the second of its slots where the block begins within its share
+  auto row_of = [&](uint32_t w) { return (2 * (size_t)w + (w == c.from ? 1 : 0)) * ROWS + i; };
   constexpr int N = DC / 64;
   float m = -INFINITY, l = 0, acc[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) acc[j] = 0;
-  for (uint32_t w = from; w <= last; ++w) {
-    const uint64_t x0 = max(share * w, p.before), x1 = min(min(share * (w + 1), p.before + p.size), all_work);
-    uint32_t t0, t1, n;
-    tiles_of<ROWS>(a, p, x0, x1, &t0, &t1, &n);
-    if (t0 == t1 || (t0 == 0 && t1 == n)) {
-      if (t0 != t1) return;  // one workgroup had all its tiles and wrote the result
-      continue;
+  for (uint32_t w0 = c.from; w0 <= c.last; w0 += 64) {  // 64 pieces at a time: a lane the maximum and sum of one
+    const uint32_t w = w0 + lane, n = min(c.last - w0 + 1, 64u);
+    float pm = -INFINITY, pl = 0;
+    if (w <= c.last) {
+      const f32x2 ml = *(const f32x2 *)(a.part_ml + 2 * row_of(w));
+      pm = ml[0];
+      pl = ml[1];
     }
-    const size_t row = (2 * (size_t)w + (share * w > p.before ? 0 : 1)) * ROWS + i;
-    const float pm = a.part_ml[2 * row], pl = a.part_ml[2 * row + 1];
-    const float top = fmaxf(m, pm), f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top), g = pm == top ? 1.0f : __builtin_amdgcn_exp2f(pm - top);
-    const float *src = a.part_acc + row * DC + lane * N;
+    float top = pm;
 #pragma unroll
-    for (int j = 0; j < N; j += 4) {
-      const f32x4 y = *(const f32x4 *)(src + j);
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    top = fmaxf(top, m);
+    const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top), g = pm == top ? 1.0f : __builtin_amdgcn_exp2f(pm - top);
+    float sum = pl * g;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) acc[j + k] = acc[j + k] * f + y[k] * g;
-    }
-    l = l * f + pl * g;
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    l = l * f + sum;
     m = top;
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] *= f;
+    const uint64_t there = __ballot(pl != 0);  // a piece of no weight has no sums
+    for (uint32_t k = 0; k < n; ++k) {
+      const float gk = __shfl(g, (int)k);
+      if (!(there >> k & 1)) continue;
+      const float *src = a.part_acc + row_of(w0 + k) * DC + lane * N;
+#pragma unroll
+      for (int j = 0; j < N; j += 4) {
+        const f32x4 y = *(const f32x4 *)(src + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j + e] = __builtin_fmaf(y[e], gk, acc[j + e]);
+      }
+    }
   }
   const float f = l > 0 ? 1.0f / l : l == 0 ? 0.0f : NAN;
-  Value *out = (Value *)a.out + (int64_t)(p.q.first + (int32_t)tok) * a.out_row + (int64_t)head * a.out_head + lane * N;
+  Value *out = (Value *)a.out + (int64_t)(c.first + (int32_t)tok) * a.out_row + (int64_t)head * a.out_head + lane * N;
   Value y[N] __attribute__((aligned(16)));
 #pragma unroll
   for (int j = 0; j < N; ++j) y[j] = (Value)(acc[j] * f);
@@ -740,7 +852,7 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
 #pragma unroll
     for (int j = 0; j < N; ++j) out[j] = y[j];
   }
-  if (lane == 0 && a.lse) a.lse[(size_t)(p.q.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+  if (lane == 0 && a.lse) a.lse[(size_t)(c.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 
 }  // namespace uzip_kv

@@ -14,13 +14,14 @@ static uzip_status launch(LatentCall &c) {
   LatentArgs &a = c.a;
   const auto kernel = latent_kernel<T, CODE, LATENT_DIM, RG>;
   // At most how much work there is: blocks, and the tiles of each.
-  const uint64_t rows = (uint64_t)a.n_rows * a.heads, blocks = rows / L::kRows + a.n_reqs + 1;
-  const uint64_t tiles = ((uint64_t)a.max_pages << a.page_shift) / kTile + 2;
-  a.groups = (uint32_t)std::min<uint64_t>(c.units, std::max<uint64_t>(1, (std::min(blocks, rows) * tiles + L::kMin - 1) / L::kMin));
+  const uint64_t rows = (uint64_t)a.n_rows * a.heads;
+  const uint64_t blocks = std::min<uint64_t>(rows / L::kRows + a.n_reqs + 1, (uint64_t)a.n_rows * ((a.heads + L::kRows - 1) / L::kRows));
+  const uint64_t tiles = (((uint64_t)a.max_pages << a.page_shift) + kTile - 1) / kTile;
+  a.groups = (uint32_t)std::min<uint64_t>(c.units, std::max<uint64_t>(1, (blocks * (tiles + 1) + L::kMin - 1) / L::kMin));
   if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(typename L::Lds)) != hipSuccess) return UZIP_EHIP;
   kernel<<<a.groups, L::kThreads, sizeof(typename L::Lds), c.stream>>>(a);
   if (a.groups > 1)
-    latent_join_kernel<T, LATENT_DIM, L::kRows, L::kMin><<<dim3(a.groups - 1, L::kRows / 4), 256, 0, c.stream>>>(a);
+    latent_join_kernel<T, LATENT_DIM, L::kRows><<<dim3(a.groups - 1, L::kRows / 4), 256, 0, c.stream>>>(a);
   return hipGetLastError() == hipSuccess ? UZIP_OK : UZIP_EHIP;
 }
 

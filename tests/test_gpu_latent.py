@@ -2,7 +2,7 @@
 
 Tolerance of an output: its own rounding (half an ulp); its weights, which enter the second product in terms of
 four bits each, 8 bits for bf16 and 12 for fp16 (expanded form: as one number of the type, 8 and 11 bits), with the last
-term's least step below that (`floor`, in units of the largest weight: 2^-19 and 2^-23; expanded fp16 2^-25); the 8-bit
+term's least step below that (`floor`, in units of the largest weight: 2^-17 and 2^-21; expanded fp16 2^-25); the 8-bit
 matrix instruction, which drops what lies 2^-13 below the largest of eight products: for each of eight at most
 that, 2^-10 of the sum of magnitudes; the scores, by their products' sums (width * 2^-24 of the sum of magnitudes), the
 exponential (2^-22 of the score and 2^-21) and the token's exponent added to them (2^-23 of it), twice, in numerator
@@ -21,7 +21,7 @@ from test_gpu_rotary import LEAST, TYPES, U_OUT, check as check_turned, dev, fre
 pytestmark = pytest.mark.gpu
 
 U_P = {"bf16": 2.0 ** -8 + 2.0 ** -10, "fp16": 2.0 ** -12 + 2.0 ** -10}
-FLOOR = {"bf16": 2.0 ** -19, "fp16": 2.0 ** -23}
+FLOOR = {"bf16": 2.0 ** -17, "fp16": 2.0 ** -21}
 U_EXPANDED = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
 FLOOR_EXPANDED = {"bf16": 0.0, "fp16": 2.0 ** -25}
 
