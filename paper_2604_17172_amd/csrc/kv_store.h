@@ -64,7 +64,7 @@ struct Eight {
 
 // The codes of places 0 .. off - 1 again, where the page's scale grew.
 template <int CODE>
-__device__ void grow_page(uint8_t *codes, bool values, uint32_t off, uint32_t D, uint32_t P, uint32_t was, uint32_t e,
+__device__ __forceinline__ void grow_page(uint8_t *codes, bool values, uint32_t off, uint32_t D, uint32_t P, uint32_t was, uint32_t e,
                           uint32_t tid, uint32_t threads) {
   const float down = pow2(max(127 + (int)was - (int)e, 0));
   for (uint32_t i = tid; i < off * D; i += threads) {
@@ -74,7 +74,7 @@ __device__ void grow_page(uint8_t *codes, bool values, uint32_t off, uint32_t D,
 }
 
 template <int T, int CODE, int THREADS, bool VALUES>
-__device__ void store_run(const StoreArgs &a, uint32_t run, uint32_t h, uint32_t tid, float *part, uint32_t *odd_part) {
+__device__ __forceinline__ void store_run(const StoreArgs &a, uint32_t run, uint32_t h, uint32_t tid, float *part, uint32_t *odd_part) {
   typedef typename Elem<T>::type Value;
   const uint32_t D = a.c.dim, P = a.c.page, per = D / 8;
   const int32_t row = a.runs[2 * (size_t)run];
@@ -229,7 +229,7 @@ __device__ void store_run(const StoreArgs &a, uint32_t run, uint32_t h, uint32_t
 // A run of one row by a wave: every lane a channel or a few, nothing but the row
 // number needed to ask for them.  64 rows of 8 heads: 4.0 us, by workgroups 6.5.
 template <int T, int CODE>
-__device__ void store_one(const StoreArgs &a, bool values, int32_t row, uint32_t h, uint32_t lane) {
+__device__ __forceinline__ void store_one(const StoreArgs &a, bool values, int32_t row, uint32_t h, uint32_t lane) {
   typedef typename Elem<T>::type Value;
   const uint32_t D = a.c.dim, P = a.c.page;
   const Value *x = (const Value *)a.x[values] + (int64_t)row * a.row[values] + (int64_t)h * a.head[values];

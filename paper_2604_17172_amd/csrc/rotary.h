@@ -64,31 +64,65 @@ __device__ __forceinline__ uint32_t channel_of(const Turn &t, uint32_t p, uint32
   return r < t.first ? r : r + 2 * t.half;
 }
 
-// A unit: pairs 8 u .. 8 u + 7.  With `even` its sixteen channels are two groups of eight; the
-// first channel of each.
+// A unit: pairs W u .. W u + W - 1.  Where half and first are multiples of W its channels are two
+// groups of W; the first channel of each.
 struct Groups {
   uint32_t a, b;
   bool turned;
 };
+template <int W>
 __device__ __forceinline__ Groups groups_of(const Turn &t, uint32_t u) {
-  if (8 * u < t.half) {
-    const uint32_t a = t.first + (t.interleaved ? 16 * u : 8 * u);
-    return {a, t.interleaved ? a + 8 : a + t.half, true};
+  if (W * u < t.half) {
+    const uint32_t a = t.first + (t.interleaved ? 2 * W * u : W * u);
+    return {a, t.interleaved ? a + W : a + t.half, true};
   }
-  const uint32_t r = 16 * u - 2 * t.half;
-  return {r < t.first ? r : r + 2 * t.half, r + 8 < t.first ? r + 8 : r + 8 + 2 * t.half, false};
+  const uint32_t r = 2 * W * u - 2 * t.half;
+  return {r < t.first ? r : r + 2 * t.half, r + W < t.first ? r + W : r + W + 2 * t.half, false};
 }
 
-// Turns a unit's sixteen values (two groups of eight), rot(j) the turn of its pair j.
-template <class F>
+// Turns a unit's values (two groups of W), rot(j) the turn of its pair j.  The two orders are two loops: as one
+// with a choice inside, the values are reached through a chosen address and no longer stay in registers.
+template <int W, class F>
 __device__ __forceinline__ void turn_unit(const Turn &t, float *x, const F &rot) {
+  if (t.interleaved) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const CosSin r = rot(j);
-    if (t.interleaved) turn_pair(r, x[2 * j], x[2 * j + 1]);
-    else turn_pair(r, x[j], x[j + 8]);
+    for (int j = 0; j < W; ++j) turn_pair(rot(j), x[2 * j], x[2 * j + 1]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j) turn_pair(rot(j), x[j], x[j + W]);
   }
 }
+
+// W values that lie side by side, at a multiple of their bytes.
+template <int T, int W>
+struct Piece {
+  typedef typename Elem<T>::type Value;
+  typedef uint32_t Words __attribute__((ext_vector_type(W * sizeof(Value) / 4)));
+  Words w;
+  __device__ __forceinline__ void load(const Value *x) { w = *(const Words *)x; }
+  __device__ __forceinline__ void store(Value *x) const { *(Words *)x = w; }
+  __device__ __forceinline__ void get(float *x) const {
+    Value v[W];
+    __builtin_memcpy(v, &w, sizeof(w));
+#pragma unroll
+    for (int j = 0; j < W; ++j) x[j] = (float)v[j];
+  }
+  __device__ __forceinline__ void put(const float *x) {
+    Value v[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[j] = (Value)x[j];
+    __builtin_memcpy(&w, v, sizeof(w));
+  }
+};
+template <int T>
+struct Piece<T, 1> {
+  typedef typename Elem<T>::type Value;
+  Value w;
+  __device__ __forceinline__ void load(const Value *x) { w = *x; }
+  __device__ __forceinline__ void store(Value *x) const { *x = w; }
+  __device__ __forceinline__ void get(float *x) const { *x = (float)w; }
+  __device__ __forceinline__ void put(const float *x) { w = (Value)*x; }
+};
 
 // Division by a number known on the host, of n < 2^31.
 struct FastDiv {
@@ -109,9 +143,9 @@ struct TurnRows {
   int64_t x_row, x_head, out_row, out_head;
   uint32_t n_rows, heads, dim;
   uint32_t block_rows;  // rows of a workgroup
-  uint32_t units;       // of a head, ceil(dim / 16)
+  uint32_t width;       // pairs of a unit: what 16 bytes hold, 4, or 1
+  uint32_t units;       // of a head, ceil(dim / 2 / width)
   FastDiv by_units, by_heads, by_half;
-  bool vec;             // rows start at multiples of 16 bytes, in whole groups of eight
   bool in_place;        // out is x: what is not turned stays where it is
 };
 
@@ -119,56 +153,66 @@ constexpr int kTurnThreads = 256;
 constexpr uint32_t kTurnTable = 1024;  // turns that a workgroup holds, at most: 8 KiB
 
 // One workgroup's rows.  The turns of a row are the same for all its heads: they are
-// worked out once, into LDS.
-template <int T>
-__device__ __forceinline__ void turn_rows(const TurnRows &a, const Turn &t, uint32_t block, CosSin *table) {
+// worked out once, into LDS, while the first values are on their way.  Bound by the rows' bytes: 16384 rows of
+// 32 heads of 128 in bf16, 268 MB in 44 us, 6.1 TB/s.  Units of four pairs keep wide loads where the rotary part
+// is no multiple of 8: 4099 rows of 11 heads of 104 in fp32, 40 of them turned, 37.5 MB in 8.3 us (pair by
+// pair: 34.5 us).
+template <int T, int W>
+__device__ __forceinline__ void turn_units(const TurnRows &a, const Turn &t, uint32_t block, CosSin *table) {
   typedef typename Elem<T>::type Value;
   const uint32_t r0 = block * a.block_rows, rows = min(a.block_rows, a.n_rows - r0), tid = threadIdx.x;
+  const uint32_t per_row = a.units * a.heads, count = rows * per_row;
+  struct Unit {
+    Piece<T, W> a, b;
+    Groups g;
+    Value *out;
+    uint32_t turns;  // place of its first in the table
+  };
+  auto fetch = [&](uint32_t i) {
+    const uint32_t rh = a.by_units.div(i), u = i - rh * a.units, r = a.by_heads.div(rh), h = rh - r * a.heads;
+    Unit n;
+    n.g = groups_of<W>(t, u);
+    n.out = (Value *)a.out + (int64_t)(r0 + r) * a.out_row + (int64_t)h * a.out_head;
+    n.turns = r * t.half + W * u;
+    if (n.g.turned || !a.in_place) {
+      const Value *x = (const Value *)a.x + (int64_t)(r0 + r) * a.x_row + (int64_t)h * a.x_head;
+      n.a.load(x + n.g.a);
+      if (n.g.b < a.dim) n.b.load(x + n.g.b);
+    }
+    return n;
+  };
+  Unit now;
+  if (tid < count) now = fetch(tid);
   for (uint32_t i = tid; i < rows * t.half; i += kTurnThreads) {
     const uint32_t r = a.by_half.div(i);
     table[i] = turn_of(t, t.positions[r0 + r], i - r * t.half);
   }
   __syncthreads();
-  const uint32_t per_row = a.units * a.heads;
-  for (uint32_t i = tid; i < rows * per_row; i += kTurnThreads) {
-    const uint32_t rh = a.by_units.div(i), u = i - rh * a.units, r = a.by_heads.div(rh), h = rh - r * a.heads;
-    const Value *x = (const Value *)a.x + (int64_t)(r0 + r) * a.x_row + (int64_t)h * a.x_head;
-    Value *out = (Value *)a.out + (int64_t)(r0 + r) * a.out_row + (int64_t)h * a.out_head;
-    const CosSin *row = table + r * t.half;
-    if (a.vec) {
-      const Groups g = groups_of(t, u);
-      if (!g.turned && a.in_place) continue;
-      Eight<T> e[2];
-      e[0].load(x + g.a, true);
-      if (g.b < a.dim) e[1].load(x + g.b, true);
-      if (g.turned) {
-        float v[16];
-        e[0].get(v);
-        e[1].get(v + 8);
-        turn_unit(t, v, [&](int j) { return row[8 * u + j]; });
-        e[0].put(v);
-        e[1].put(v + 8);
-      }
-      e[0].store(out + g.a);
-      if (g.b < a.dim) e[1].store(out + g.b);
-    } else {
-#pragma unroll 1
-      for (uint32_t p = 8 * u; p < 8 * u + 8; ++p) {
-        const uint32_t ca = channel_of(t, p, 0), cb = channel_of(t, p, 1);
-        if (ca >= a.dim || (p >= t.half && a.in_place)) break;
-        if (p < t.half) {
-          float va = (float)x[ca], vb = (float)x[cb];
-          turn_pair(row[p], va, vb);
-          out[ca] = (Value)va;
-          out[cb] = (Value)vb;
-        } else {
-          const Value va = x[ca];
-          if (cb < a.dim) out[cb] = x[cb];
-          out[ca] = va;
-        }
-      }
+  for (uint32_t i = tid; i < count; i += kTurnThreads) {
+    Unit next;
+    if (i + kTurnThreads < count) next = fetch(i + kTurnThreads);
+    if (now.g.turned) {
+      float v[2 * W];
+      now.a.get(v);
+      now.b.get(v + W);
+      turn_unit<W>(t, v, [&](int j) { return table[now.turns + j]; });
+      now.a.put(v);
+      now.b.put(v + W);
     }
+    if (now.g.turned || !a.in_place) {
+      now.a.store(now.out + now.g.a);
+      if (now.g.b < a.dim) now.b.store(now.out + now.g.b);
+    }
+    now = next;
   }
+}
+
+template <int T>
+__device__ __forceinline__ void turn_rows(const TurnRows &a, const Turn &t, uint32_t block, CosSin *table) {
+  constexpr int kWide = 16 / sizeof(typename Elem<T>::type);
+  if (a.width == kWide) turn_units<T, kWide>(a, t, block, table);
+  else if (kWide != 4 && a.width == 4) turn_units<T, 4>(a, t, block, table);
+  else turn_units<T, 1>(a, t, block, table);
 }
 
 // ------------------------------------------------------------------ host
@@ -190,15 +234,19 @@ inline bool rows_to_turn(uzip_dtype dtype, const void *x, int64_t x_row, int64_t
   if (heads == 0 || heads > 65535 || dim > 1024 || t->first + t->rot > dim || !valid_rows(x, x_row, x_head, bytes) ||
       !valid_rows(out, out_row, out_head, bytes) || n_rows > UZIP_KV_MAX_ROWS || (uint64_t)n_rows * heads > UZIP_KV_MAX_ROW_HEADS)
     return false;
-  auto whole = [&](const void *p, int64_t row, int64_t head) { return aligned(p, 16) && row * bytes % 16 == 0 && head * bytes % 16 == 0; };
-  const uint32_t half = t->rot / 2, units = (dim + 15) / 16, per_row = units * heads;
+  const uint32_t half = t->rot / 2;
+  auto fits = [&](uint32_t w) {
+    const uint32_t size = w * bytes;
+    return (half | t->first | dim) % w == 0 && aligned(x, size) && aligned(out, size) && ((x_row | x_head | out_row | out_head) & (w - 1)) == 0;
+  };
+  const uint32_t width = fits(16 / bytes) ? 16 / bytes : fits(4) ? 4 : 1;
+  const uint32_t units = ((dim + 1) / 2 + width - 1) / width, per_row = units * heads;
   // Rows of a workgroup: four units to a thread, as long as there are rows for every compute unit and
   // the table holds their turns.
   uint32_t rows = 1;
   while (rows * per_row < 4 * kTurnThreads && 2 * rows * half <= kTurnTable && n_rows > 512 * rows) rows *= 2;
-  *a = {x, out, x_row, x_head, out_row, out_head, n_rows, heads, dim, rows, units, FastDiv::of(units), FastDiv::of(heads), FastDiv::of(half),
-        half % 8 == 0 && t->first % 8 == 0 && dim % 8 == 0 && whole(x, x_row, x_head) && whole(out, out_row, out_head),
-        out == x && out_row == x_row && out_head == x_head};
+  *a = {x, out, x_row, x_head, out_row, out_head, n_rows, heads, dim, rows, width, units, FastDiv::of(units), FastDiv::of(heads),
+        FastDiv::of(half), out == x && out_row == x_row && out_head == x_head};
   return true;
 }
 inline uint32_t turn_blocks(const TurnRows &a) { return a.block_rows ? (a.n_rows + a.block_rows - 1) / a.block_rows : 0; }
