@@ -29,8 +29,8 @@ HIPCC_FLAGS = [
     "-Wall", "-Wno-unused-command-line-argument",
 ]
 
-# Sources whose matrix instructions accumulate in vector registers: their sums are also rescaled, and
-# would move to the accumulation registers and back each time (a third of the loop's instructions).
+# Sources whose matrix instructions accumulate in vector registers: a tile's scores are read by vector instructions at once,
+# and would move there from the accumulation registers (a fifth of the loop's instructions).
 SOURCE_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
                 for name in ("expanded_64.hip", "expanded_128.hip")}
 

@@ -12,7 +12,8 @@ struct ExpandedCall {
   ExpandedArgs a;
   uzip_dtype type;
   uint32_t rot, value;
-  bool few;  // blocks of 32 rows
+  uint32_t rows;  // of a workgroup
+  bool direct;    // keys and values can go to LDS as they are
   hipStream_t stream;
 };
 

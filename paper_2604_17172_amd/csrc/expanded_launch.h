@@ -5,10 +5,10 @@
 
 namespace uzip_kv {
 
-template <int T, int DR, int DV, int WAVES>
+template <int T, int DR, int DV, int R, int RG, int SPLIT, bool DIRECT>
 static uzip_status launch(const ExpandedCall &c) {
-  typedef Expanded<EXPANDED_NOPE, DR, DV, WAVES> L;
-  const auto kernel = expanded_kernel<T, EXPANDED_NOPE, DR, DV, WAVES>;
+  typedef Expanded<EXPANDED_NOPE, DR, DV, R, RG, SPLIT> L;
+  const auto kernel = expanded_kernel<T, EXPANDED_NOPE, DR, DV, R, RG, SPLIT, DIRECT>;
   // blocks: full ones, and a last one for each request and for the rows of none
   const uint64_t blocks = std::min<uint64_t>(c.a.n_rows, (uint64_t)c.a.n_rows / L::kRows + c.a.n_reqs + 1);
   if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(typename L::Lds)) != hipSuccess)
@@ -18,7 +18,8 @@ static uzip_status launch(const ExpandedCall &c) {
 }
 template <int T, int DR, int DV>
 static uzip_status launch(const ExpandedCall &c) {
-  return c.few ? launch<T, DR, DV, 1>(c) : launch<T, DR, DV, 4>(c);
+  if (!c.direct) return launch<T, DR, DV, 1, 1, 4, false>(c);
+  return c.rows == 32 ? launch<T, DR, DV, 1, 1, 4, true>(c) : c.rows == 64 ? launch<T, DR, DV, 2, 1, 4, true>(c) : launch<T, DR, DV, 2, 2, 2, true>(c);
 }
 template <int T>
 static uzip_status launch(const ExpandedCall &c) {
