@@ -27,10 +27,19 @@ __device__ __forceinline__ float finite_or_zero(float x) {
   const float f = fabsf(x);
   return f < INFINITY ? f : 0.0f;
 }
+// The largest of a wave, in all lanes: within rows of 16 lanes, then the rows.  By cross-lane moves of the vector
+// unit: the twelve exchanges of two such maxima over LDS took half of a store's time.
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-  return x;
+  auto moved = [](float y, auto control) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(y), decltype(control)::value, 0xf, 0xf, true));
+  };
+  x = fmaxf(x, moved(x, std::integral_constant<int, 0xB1>{}));   // lanes 1 0 3 2 of each four
+  x = fmaxf(x, moved(x, std::integral_constant<int, 0x4E>{}));   // 2 3 0 1
+  x = fmaxf(x, moved(x, std::integral_constant<int, 0x124>{}));  // row turned by 4
+  x = fmaxf(x, moved(x, std::integral_constant<int, 0x128>{}));  // by 8
+  const uint32_t w = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+  return max_of_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
 
 template <int T, int CODE>
@@ -58,15 +67,24 @@ __device__ void store_latent(const LatentStoreArgs &a, const Turn &t, uint32_t r
   }
   if (slot < 0 || (uint64_t)slot >= a.n_slots) return;
   float most = 0;
+  bool odd = false;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) most = fmaxf(most, finite_or_zero(v[j]));
+  for (int j = 0; j < 8; ++j) {
+    const float f = finite_or_zero(v[j]);
+    odd = odd || f != fabsf(v[j]);
+    most = fmaxf(most, f);
+  }
   const int ec = exponent_for<CODE>(wave_max(most));
   const int er = exponent_for<CODE>(wave_max(fmaxf(finite_or_zero(ra), finite_or_zero(rb))));
   const float inv = pow2(254 - ec), inv_r = pow2(254 - er);
   uint8_t *to = a.codes + (size_t)slot * (C + R);
   u32x2 w = {0, 0};
+  if (odd || ec >= Code<CODE>::kExpMax) {  // there values may lie past the largest code
 #pragma unroll
-  for (int j = 0; j < 8; ++j) w[j / 4] |= encode<CODE>(v[j], inv) << (8 * (j % 4));
+    for (int j = 0; j < 8; ++j) w[j / 4] |= encode<CODE>(v[j], inv) << (8 * (j % 4));
+  } else {
+    w = u32x2{encode4<CODE>(v, inv), encode4<CODE>(v + 4, inv)};
+  }
   if (per == 8) *(u32x2 *)(to + 8 * lane) = w;
   else *(uint32_t *)(to + 4 * lane) = w.x;
   if (lane < t.half) {

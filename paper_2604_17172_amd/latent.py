@@ -83,14 +83,17 @@ def _current(cache: LatentCache) -> int:
 
 
 def _serves(*tensors) -> None:
-    if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in tensors):
-        raise ValueError("no gradient goes through this call: detach its inputs, or call it under torch.no_grad()")
+    if torch.is_grad_enabled():
+        for x in tensors:
+            if x is not None and x.requires_grad:
+                raise ValueError("no gradient goes through this call: detach its inputs, or call it under torch.no_grad()")
 
 
 def _vectors(x: torch.Tensor, name: str, dim: int, device: int) -> int:
-    if x.dim() != 2:
-        raise ValueError(f"{name} is [rows, {dim}]")
-    return _rows(x[:, None], name, dim, device)
+    t = _TYPES.get(x.dtype)
+    if t is None or x.get_device() != device or x.dim() != 2 or x.shape[1] != dim or (x.stride(1) != 1 and x.numel()):
+        raise ValueError(f"{name} is [rows, {dim}] in bf16, fp16 or fp32 on the current GPU with each row's values side by side")
+    return t
 
 
 def latent_store(cache: LatentCache, latent: torch.Tensor, key_rot: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor,
