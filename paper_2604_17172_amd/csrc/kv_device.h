@@ -106,4 +106,16 @@ struct Elem<UZIP_FP32> {
   typedef float type;
 };
 
+// Division by a number known on the host, of n < 2^31.
+struct FastDiv {
+  uint32_t d, m, s;
+  static FastDiv of(uint32_t d) {
+    FastDiv f{d, 0, 0};
+    while ((1ull << f.s) < d) ++f.s;
+    f.m = (uint32_t)((((1ull << f.s) - d) << 32) / d + 1);
+    return f;
+  }
+  __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
+};
+
 }  // namespace uzip_kv

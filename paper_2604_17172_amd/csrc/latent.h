@@ -44,6 +44,8 @@ struct LatentArgs {
   uint32_t n_pages, page_shift, rot;
   uint32_t n_rows, heads, max_pages, n_reqs;
   uint32_t groups;    // workgroups that the work is shared by
+  FastDiv by_heads;
+  double growth;      // by which a request's blocks grow from one to the next, in tiles
   float scale_log2;   // scale log2 e
   bool q_vec, out_vec;
 };
@@ -72,14 +74,14 @@ __device__ __forceinline__ LatentRequest latent_request(const LatentArgs &a, uin
 
 // The work of a request's first b blocks of ROWS rows, in tiles: each block one for its beginning and end,
 // and the tiles that its last row sees, which grow by ROWS / heads tokens from block to block.
-// It only has to be the same everywhere; a block's real tiles are spread over its share.
+// It only has to grow with b and be the same everywhere; a block's real tiles are spread over its share.  (Divisions of
+// 64-bit numbers by such took 3 us of a workgroup's beginning: here and below they are of doubles, set right where
+// the quotient has to be exact.)
 template <int ROWS>
 __device__ __forceinline__ uint64_t work_before(const LatentArgs &a, const LatentRequest &q, uint32_t b) {
-  const int32_t seen = min(max(q.base + (int32_t)((min((uint32_t)q.rows * a.heads, (uint32_t)ROWS) - 1) / a.heads) + 1, 0), q.len);
+  const int32_t seen = min(max(q.base + (int32_t)a.by_heads.div(min((uint32_t)q.rows * a.heads, (uint32_t)ROWS) - 1) + 1, 0), q.len);
   const uint64_t first = 1 + ((uint32_t)seen + kTile - 1) / kTile;
-  uint64_t more = (uint64_t)b * (b - 1) / 2;
-  if (b < 2) more = 0;
-  return b * first + more * ROWS / (kTile * a.heads);
+  return b * first + (b < 2 ? 0 : (uint64_t)((double)((uint64_t)b * (b - 1) / 2) * a.growth));
 }
 template <int ROWS>
 __device__ __forceinline__ uint32_t blocks_of(const LatentArgs &a, const LatentRequest &q) {
@@ -92,19 +94,27 @@ struct Place {
   uint32_t req, block, blocks;
   uint64_t before, size;  // of the block, in the call's work
 };
-__device__ __forceinline__ uint64_t wave_sum(uint64_t x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+// n / d, rounded down, both below 2^52
+__device__ __forceinline__ uint64_t quotient(uint64_t n, uint64_t d) {
+  uint64_t q = (uint64_t)((double)n / (double)d);
+  if (q * d > n) --q;
+  return q;
 }
-__device__ __forceinline__ uint64_t wave_before(uint64_t x) {  // sum over the lanes before this one
-  uint64_t s = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t y = __shfl_up(s, o);
-    if ((int)(threadIdx.x & 63) >= o) s += y;
-  }
-  return s - x;
+// The sum over the lanes up to and with this one: by moves between neighbouring lanes, then from rows of 16 lanes to the next.
+__device__ __forceinline__ uint64_t wave_upto(uint64_t x) {
+  auto add = [&](auto control, auto rows) {
+    const uint32_t low = __builtin_amdgcn_update_dpp(0, (uint32_t)x, decltype(control)::value, decltype(rows)::value, 0xf, false);
+    const uint32_t high = __builtin_amdgcn_update_dpp(0, (uint32_t)(x >> 32), decltype(control)::value, decltype(rows)::value, 0xf, false);
+    x += (uint64_t)high << 32 | low;
+  };
+  typedef std::integral_constant<int, 0xf> Every;
+  add(std::integral_constant<int, 0x111>{}, Every{});  // from the lane 1 before, of the row
+  add(std::integral_constant<int, 0x112>{}, Every{});  // 2
+  add(std::integral_constant<int, 0x114>{}, Every{});  // 4
+  add(std::integral_constant<int, 0x118>{}, Every{});  // 8
+  add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // lane 15 to row 1, 47 to row 3
+  add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // lane 31 to rows 2 and 3
+  return x;
 }
 
 template <int ROWS>
@@ -122,19 +132,20 @@ __device__ bool find_block(const LatentArgs &a, const F &x_of, Place *out) {
   const uint32_t lane = threadIdx.x & 63, n = a.n_reqs + 1;
   const uint32_t each = (n + 63) / 64, lo = min(n, lane * each), hi = min(n, lo + each);
   uint64_t mine = 0;
+  Place p{};
   for (uint32_t i = lo; i < hi; ++i) {
-    const LatentRequest q = latent_request(a, i);
-    if (q.rows > 0) mine += work_before<ROWS>(a, q, blocks_of<ROWS>(a, q));
+    p.q = latent_request(a, i);
+    if (p.q.rows > 0) mine += work_before<ROWS>(a, p.q, blocks_of<ROWS>(a, p.q));
   }
-  const uint64_t all = wave_sum(mine), before = wave_before(mine);
+  const uint64_t upto = wave_upto(mine), before = upto - mine;
+  const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(upto >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)upto, 63);
   uint64_t x;
   if (!x_of(all, &x) || x >= all) return false;
-  Place p{};
   const bool here = x >= before && x - before < mine;
   if (here) {
     uint64_t at = before;
     for (uint32_t i = lo; i < hi; ++i) {
-      p.q = latent_request(a, i);
+      if (each > 1) p.q = latent_request(a, i);
       if (p.q.rows <= 0) continue;
       p.blocks = blocks_of<ROWS>(a, p.q);
       const uint64_t size = work_before<ROWS>(a, p.q, p.blocks);
@@ -204,7 +215,7 @@ __device__ __forceinline__ bool next_block(const LatentArgs &a, Place *p) {
 // A workgroup's share of all work; shares are consecutive.
 template <int MIN>
 __device__ __forceinline__ uint64_t share_of(const LatentArgs &a, uint64_t all) {
-  const uint64_t each = (all + a.groups - 1) / a.groups;
+  const uint64_t each = quotient(all + a.groups - 1, a.groups);
   return each > MIN ? each : MIN;
 }
 
@@ -212,10 +223,11 @@ __device__ __forceinline__ uint64_t share_of(const LatentArgs &a, uint64_t all) 
 template <int ROWS>
 __device__ __forceinline__ void tiles_of(const LatentArgs &a, const Place &p, uint64_t x0, uint64_t x1, uint32_t *t0, uint32_t *t1, uint32_t *all) {
   const uint32_t list = (uint32_t)p.q.rows * a.heads, r1 = min(list, (p.block + 1) * ROWS);
-  const int32_t seen = min(max(p.q.base + (int32_t)((r1 - 1) / a.heads) + 1, 0), p.q.len);
+  const int32_t seen = min(max(p.q.base + (int32_t)a.by_heads.div(r1 - 1) + 1, 0), p.q.len);
   *all = ((uint32_t)seen + kTile - 1) / kTile;
-  *t0 = (uint32_t)((x0 - p.before) * *all / p.size);
-  *t1 = (uint32_t)((x1 - p.before) * *all / p.size);
+  // rounded alike on both sides of a share's end; all of it gives *all itself
+  *t0 = (uint32_t)((double)((x0 - p.before) * *all) / (double)p.size);
+  *t1 = (uint32_t)((double)((x1 - p.before) * *all) / (double)p.size);
 }
 
 // ------------------------------------------------------------------ the kernel
@@ -417,7 +429,7 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
     const uint32_t list = (uint32_t)q.rows * a.heads, r0 = place.block * L::kRows;
     const uint32_t rounds = tile1 - tile0;
     if (!whole && x == place.before && threadIdx.x == 0)
-      a.cuts[blockIdx.x] = {1, q.first, r0, min(list - r0, (uint32_t)L::kRows), (uint32_t)blockIdx.x, (uint32_t)((place.before + place.size - 1) / (end - begin))};
+      a.cuts[blockIdx.x] = {1, q.first, r0, min(list - r0, (uint32_t)L::kRows), (uint32_t)blockIdx.x, (uint32_t)quotient(place.before + place.size - 1, end - begin)};
 
     for (int careful = 0;; careful = 1) {
       bool again;
@@ -429,9 +441,9 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
         // ---------------------------------------------------------------- scores
         const uint32_t r = r0 + 32 * rg + col;
         const bool here = r < list;
-        const uint32_t tok = here ? r / a.heads : 0, head = here ? r - tok * a.heads : 0;
+        const uint32_t tok = here ? a.by_heads.div(r) : 0, head = here ? r - tok * a.heads : 0;
         const int32_t at = here ? q.base + (int32_t)tok : -1;                                  // the row's place
-        const int32_t at_min = q.base + (int32_t)(min(r0 + 32 * rg, list - 1) / a.heads);      // the first of the wave's rows
+        const int32_t at_min = q.base + (int32_t)a.by_heads.div(min(r0 + 32 * rg, list - 1));      // the first of the wave's rows
         const float scale_log2 = a.scale_log2;
         Eight query[2 * L::kSteps + 4];
         {
@@ -740,7 +752,7 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
         __syncthreads();
         again = !careful && lds.trouble != 0;
         const uint32_t col = only_here(threadIdx.x & 31), h = only_here(threadIdx.x & 63) >> 5, r = r0 + 32 * rg + col;
-        const uint32_t tok = r / a.heads, head = r - tok * a.heads;
+        const uint32_t tok = a.by_heads.div(r), head = r - tok * a.heads;
         float l = lds.l[rg][0][col] + lds.l[rg][1][col];
         const float m = lds.m[rg][col];
         if (careful && q.base + (int32_t)tok >= lds.first_bad) l = NAN;
@@ -800,7 +812,7 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
   const LatentCut c = a.cuts[blockIdx.x];
   const uint32_t lane = threadIdx.x & 63, i = blockIdx.y * 4 + (threadIdx.x >> 6);
   if (!c.cut || i >= c.rows) return;
-  const uint32_t r = c.r0 + i, tok = r / a.heads, head = r - tok * a.heads;
+  const uint32_t r = c.r0 + i, tok = a.by_heads.div(r), head = r - tok * a.heads;
   // the piece of workgroup w: the second of its slots where the block begins within its share
   auto row_of = [&](uint32_t w) { return (2 * (size_t)w + (w == c.from ? 1 : 0)) * ROWS + i; };
   constexpr int N = DC / 64;
@@ -828,15 +840,21 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] *= f;
     const uint64_t there = __ballot(pl != 0);  // a piece of no weight has no sums
-    for (uint32_t k = 0; k < n; ++k) {
-      const float gk = __shfl(g, (int)k);
-      if (!(there >> k & 1)) continue;
-      const float *src = a.part_acc + row_of(w0 + k) * DC + lane * N;
+    constexpr uint32_t kAtOnce = 4;  // pieces that are read side by side
+    for (uint32_t k0 = 0; k0 < n; k0 += kAtOnce) {
+      f32x4 y[kAtOnce][N / 4];
 #pragma unroll
-      for (int j = 0; j < N; j += 4) {
-        const f32x4 y = *(const f32x4 *)(src + j);
+      for (uint32_t k = 0; k < kAtOnce; ++k) {
+        const float *src = a.part_acc + row_of(w0 + min(k0 + k, n - 1)) * DC + lane * N;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[j + e] = __builtin_fmaf(y[e], gk, acc[j + e]);
+        for (int j = 0; j < N; j += 4) y[k][j / 4] = *(const f32x4 *)(src + j);
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < kAtOnce; ++k) {
+        const float gk = __shfl(g, (int)min(k0 + k, n - 1));
+        if (k0 + k >= n || !(there >> (k0 + k) & 1)) continue;
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j] = __builtin_fmaf(y[k][j / 4][j % 4], gk, acc[j]);
       }
     }
   }

@@ -13,6 +13,8 @@ static uzip_status launch(LatentCall &c) {
   typedef Latent<T, CODE, LATENT_DIM, RG> L;
   LatentArgs &a = c.a;
   const auto kernel = latent_kernel<T, CODE, LATENT_DIM, RG>;
+  a.by_heads = FastDiv::of(a.heads);
+  a.growth = (double)L::kRows / ((double)kTile * a.heads);
   // At most how much work there is: blocks, and the tiles of each.
   const uint64_t rows = (uint64_t)a.n_rows * a.heads;
   const uint64_t blocks = std::min<uint64_t>(rows / L::kRows + a.n_reqs + 1, (uint64_t)a.n_rows * ((a.heads + L::kRows - 1) / L::kRows));
