@@ -38,12 +38,13 @@ struct LatentArgs {
   float *lse;
   int64_t q_row, q_head, out_row, out_head;
   const int32_t *table, *lens, *q_start;
-  float *part_acc;  // [slot][row][latent]
+  float *part_acc;  // [slot][32 rows][channels' half][32 channels][8 of them][lane][4]
   float *part_ml;   // [slot][row][2]
   struct LatentCut *cuts;  // of each workgroup
   uint32_t n_pages, page_shift, rot;
   uint32_t n_rows, heads, max_pages, n_reqs;
   uint32_t groups;    // workgroups that the work is shared by
+  uint32_t begin;     // what a block's beginning and end cost, in tiles
   FastDiv by_heads;
   double growth;      // by which a request's blocks grow from one to the next, in tiles
   float scale_log2;   // scale log2 e
@@ -52,7 +53,6 @@ struct LatentArgs {
 
 constexpr int kTile = 64;  // tokens
 constexpr int kAhead = 4;  // reads of the first product under way
-
 // ------------------------------------------------------------------ pieces of work
 struct LatentRequest {
   int32_t first, rows, len, base;  // first row of the step's arrays, new tokens, tokens, place of the first new one
@@ -72,7 +72,7 @@ __device__ __forceinline__ LatentRequest latent_request(const LatentArgs &a, uin
   return r;
 }
 
-// The work of a request's first b blocks of ROWS rows, in tiles: each block one for its beginning and end,
+// The work of a request's first b blocks of ROWS rows, in tiles: each block a.begin for its beginning and end,
 // and the tiles that its last row sees, which grow by ROWS / heads tokens from block to block.
 // It only has to grow with b and be the same everywhere; a block's real tiles are spread over its share.  (Divisions of
 // 64-bit numbers by such took 3 us of a workgroup's beginning: here and below they are of doubles, set right where
@@ -80,7 +80,7 @@ __device__ __forceinline__ LatentRequest latent_request(const LatentArgs &a, uin
 template <int ROWS>
 __device__ __forceinline__ uint64_t work_before(const LatentArgs &a, const LatentRequest &q, uint32_t b) {
   const int32_t seen = min(max(q.base + (int32_t)a.by_heads.div(min((uint32_t)q.rows * a.heads, (uint32_t)ROWS) - 1) + 1, 0), q.len);
-  const uint64_t first = 1 + ((uint32_t)seen + kTile - 1) / kTile;
+  const uint64_t first = a.begin + ((uint32_t)seen + kTile - 1) / kTile;
   return b * first + (b < 2 ? 0 : (uint64_t)((double)((uint64_t)b * (b - 1) / 2) * a.growth));
 }
 template <int ROWS>
@@ -213,22 +213,27 @@ __device__ __forceinline__ bool next_block(const LatentArgs &a, Place *p) {
 }
 
 // A workgroup's share of all work; shares are consecutive.
-template <int MIN>
 __device__ __forceinline__ uint64_t share_of(const LatentArgs &a, uint64_t all) {
   const uint64_t each = quotient(all + a.groups - 1, a.groups);
-  return each > MIN ? each : MIN;
+  return each > 2 * a.begin ? each : 2 * a.begin;
 }
 
-// Tiles of the block that the work from x0 to x1 (within the block's) stands for.
+// Tiles of the block that the work from x0 to x1 (within the block's) stands for.  A block's first a.begin are its
+// beginning; where a share ends within them, the block is left to the next workgroup, whose share begins there.
 template <int ROWS>
-__device__ __forceinline__ void tiles_of(const LatentArgs &a, const Place &p, uint64_t x0, uint64_t x1, uint32_t *t0, uint32_t *t1, uint32_t *all) {
+__device__ __forceinline__ void tiles_of(const LatentArgs &a, const Place &p, uint64_t x0, uint64_t x1, uint32_t *t0, uint32_t *t1) {
   const uint32_t list = (uint32_t)p.q.rows * a.heads, r1 = min(list, (p.block + 1) * ROWS);
   const int32_t seen = min(max(p.q.base + (int32_t)a.by_heads.div(r1 - 1) + 1, 0), p.q.len);
-  *all = ((uint32_t)seen + kTile - 1) / kTile;
-  // rounded alike on both sides of a share's end; all of it gives *all itself
-  *t0 = (uint32_t)((double)((x0 - p.before) * *all) / (double)p.size);
-  *t1 = (uint32_t)((double)((x1 - p.before) * *all) / (double)p.size);
+  const uint32_t all = ((uint32_t)seen + kTile - 1) / kTile;
+  // rounded alike on both sides of a share's end; all of it gives `all` itself
+  auto tiles = [&](uint64_t x) {
+    const uint64_t done = x - p.before;
+    return done <= a.begin ? 0u : done == p.size ? all : (uint32_t)((double)((done - a.begin) * all) / (double)(p.size - a.begin));
+  };
+  *t0 = tiles(x0);
+  *t1 = x1 == p.before + p.size ? all : tiles(x1);
 }
+__device__ __forceinline__ bool leaves(const LatentArgs &a, const Place &p, uint64_t end) { return end < p.before + p.size && end - p.before <= a.begin; }
 
 // ------------------------------------------------------------------ the kernel
 // One wave takes 32 rows.  Matrix instructions of 32 x 32: a lane holds, of the first operand, values of
@@ -347,7 +352,6 @@ template <int T, int CODE, int DC, int RG>
 struct Latent {
   static constexpr int kRows = 32 * RG, kThreads = 256 * RG, kBlocks = DC / 64, kSteps = DC / 32;
   static constexpr int kBufs = 3;      // tiles in LDS: one whose values are read, one whose keys are, one under way
-  static constexpr int kMin = 4;       // the least share of a workgroup
   static constexpr float kLag = 5;     // weights up to 2^5: times 2^3 they are codes
   typedef LatentTile<DC> Tile;
   struct Lds {
@@ -397,16 +401,18 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
   const bool adds = wave_of_all >= kWaves;
   const uint32_t wave = wave_of_all % kWaves, rg = wave / 2, half = wave % 2, col = lane & 31, h = lane >> 5;
   if (threadIdx.x == 0) args.cuts[blockIdx.x].cut = 0;
-  uint64_t begin = 0, end = 0;
+  uint64_t begin = 0, end = 0, share = 0;
   Place place;
   if (!find_block<L::kRows>(args, [&](uint64_t all, uint64_t *x) {
-        const uint64_t share = share_of<L::kMin>(args, all);
+        share = uniform(share_of(args, all));
         begin = uniform(share * blockIdx.x);
         end = uniform((uint64_t)min(begin + share, all));
         *x = begin;
         return begin < all;
       }, &place))
     return;
+  uniform(&place);
+  if (begin - place.before <= args.begin) begin = place.before;
 
   // what does not change from block to block
   const uint32_t lds0 = lds_at(lds_bytes), tiles0 = lds0 + (uint32_t)offsetof(typename L::Lds, tile);
@@ -416,12 +422,12 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
   // Tiles lie at multiples of 256 bytes, so that the exclusive or of an address's swizzle may come last.
   static_assert(sizeof(Tile) % 256 == 0 && offsetof(typename L::Lds, tile) % 256 == 0 && offsetof(Tile, rot) % 256 == 0, "swizzled addresses");
 
-  for (uint64_t x = begin; x < end;) {
+  for (uint64_t x = begin; x < end && !leaves(args, place, end);) {
     const LatentArgs a = read_again();
     uniform(&place);
     const uint64_t x1 = min(end, place.before + place.size);
-    uint32_t tile0, tile1, tiles_all;
-    tiles_of<L::kRows>(a, place, x, x1, &tile0, &tile1, &tiles_all);
+    uint32_t tile0, tile1;
+    tiles_of<L::kRows>(a, place, x, x1, &tile0, &tile1);
     tile0 = uniform(tile0);
     tile1 = uniform(tile1);
     const LatentRequest &q = place.q;
@@ -429,7 +435,7 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
     const uint32_t list = (uint32_t)q.rows * a.heads, r0 = place.block * L::kRows;
     const uint32_t rounds = tile1 - tile0;
     if (!whole && x == place.before && threadIdx.x == 0)
-      a.cuts[blockIdx.x] = {1, q.first, r0, min(list - r0, (uint32_t)L::kRows), (uint32_t)blockIdx.x, (uint32_t)quotient(place.before + place.size - 1, end - begin)};
+      a.cuts[blockIdx.x] = {1, q.first, r0, min(list - r0, (uint32_t)L::kRows), (uint32_t)blockIdx.x, (uint32_t)quotient(place.before + place.size - 1, share)};
 
     for (int careful = 0;; careful = 1) {
       bool again;
@@ -781,6 +787,7 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
               a.lse[(size_t)(q.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
           } else {
             const size_t slot = 2 * (size_t)blockIdx.x + (begin > place.before ? 0 : 1), row = slot * L::kRows + 32 * rg + col;
+            f32x4 *part = (f32x4 *)a.part_acc + (((slot * RG + rg) * 2 + half) * L::kBlocks * 4) * 64 + 32 * h + col;  // as the lanes hold them
 #pragma unroll
             for (int b = 0; b < L::kBlocks && rounds > 0; ++b)
 #pragma unroll
@@ -788,7 +795,7 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
                 f32x4 y;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) y[k] = acc[b][4 * g + k];
-                *(f32x4 *)(a.part_acc + row * DC + channel0 + 32 * b + 8 * g + 4 * h) = y;
+                part[(4 * b + g) * 64] = y;
               }
             if (half == 0 && h == 0) {
               a.part_ml[2 * row] = m;
@@ -804,73 +811,64 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
   }
 }
 
-// The pieces of a block that several workgroups shared.  Workgroup (w, y): four rows, a wave each, of the block that workgroup w
-// was the first of.
-template <int T, int DC, int ROWS>
+// The pieces of a block that several workgroups shared.  Workgroup (w, y): 32 rows by 32 channels, the y-th such, of the block
+// that workgroup w was the first of; a lane has what one of the adding waves' lanes had, so that pieces are read as they were
+// written, 1024 bytes at a time (row by row, they were written 16 bytes at a time: 5.6 us of a workgroup's end, now 2.9).
+template <int T, int DC, int RG>
 __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
   typedef typename Elem<T>::type Value;
+  constexpr int kBlocks = DC / 64, kRows = 32 * RG;
   const LatentCut c = a.cuts[blockIdx.x];
-  const uint32_t lane = threadIdx.x & 63, i = blockIdx.y * 4 + (threadIdx.x >> 6);
-  if (!c.cut || i >= c.rows) return;
-  const uint32_t r = c.r0 + i, tok = a.by_heads.div(r), head = r - tok * a.heads;
+  const uint32_t lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5, g = threadIdx.x >> 6;
+  const uint32_t b = blockIdx.y % kBlocks, half = blockIdx.y / kBlocks % 2, rg = blockIdx.y / kBlocks / 2, i = 32 * rg + col;
+  if (!c.cut || 32 * rg >= c.rows) return;
   // the piece of workgroup w: the second of its slots where the block begins within its share
-  auto row_of = [&](uint32_t w) { return (2 * (size_t)w + (w == c.from ? 1 : 0)) * ROWS + i; };
-  constexpr int N = DC / 64;
-  float m = -INFINITY, l = 0, acc[N];
+  auto slot_of = [&](uint32_t w) { return 2 * (size_t)w + (w == c.from ? 1 : 0); };
+  auto ml_of = [&](uint32_t w) { return *(const f32x2 *)(a.part_ml + 2 * (slot_of(w) * kRows + i)); };
+  constexpr uint32_t kAtOnce = 8;  // pieces that are read side by side
+  float m = -INFINITY, l = 0;
+  f32x4 acc = {0, 0, 0, 0};
+  for (uint32_t w0 = c.from; w0 <= c.last; w0 += kAtOnce) {
+    f32x2 ml[kAtOnce];
+    f32x4 part[kAtOnce];
 #pragma unroll
-  for (int j = 0; j < N; ++j) acc[j] = 0;
-  for (uint32_t w0 = c.from; w0 <= c.last; w0 += 64) {  // 64 pieces at a time: a lane the maximum and sum of one
-    const uint32_t w = w0 + lane, n = min(c.last - w0 + 1, 64u);
-    float pm = -INFINITY, pl = 0;
-    if (w <= c.last) {
-      const f32x2 ml = *(const f32x2 *)(a.part_ml + 2 * row_of(w));
-      pm = ml[0];
-      pl = ml[1];
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      const uint32_t w = min(w0 + k, c.last);
+      ml[k] = ml_of(w);
+      part[k] = ((const f32x4 *)a.part_acc)[((((slot_of(w) * RG + rg) * 2 + half) * kBlocks + b) * 4 + g) * 64 + lane];
     }
-    float top = pm;
+    float top = m;
 #pragma unroll
-    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    top = fmaxf(top, m);
-    const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top), g = pm == top ? 1.0f : __builtin_amdgcn_exp2f(pm - top);
-    float sum = pl * g;
+    for (uint32_t k = 0; k < kAtOnce; ++k) top = fmaxf(top, ml[k][0]);
+    const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+    l *= f;
 #pragma unroll
-    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-    l = l * f + sum;
+    for (int e = 0; e < 4; ++e) acc[e] *= f;
     m = top;
 #pragma unroll
-    for (int j = 0; j < N; ++j) acc[j] *= f;
-    const uint64_t there = __ballot(pl != 0);  // a piece of no weight has no sums
-    constexpr uint32_t kAtOnce = 4;  // pieces that are read side by side
-    for (uint32_t k0 = 0; k0 < n; k0 += kAtOnce) {
-      f32x4 y[kAtOnce][N / 4];
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      if (w0 + k > c.last || ml[k][1] == 0) continue;  // a piece of no weight has no sums
+      const float fk = ml[k][0] == top ? 1.0f : __builtin_amdgcn_exp2f(ml[k][0] - top);
+      l = __builtin_fmaf(ml[k][1], fk, l);
 #pragma unroll
-      for (uint32_t k = 0; k < kAtOnce; ++k) {
-        const float *src = a.part_acc + row_of(w0 + min(k0 + k, n - 1)) * DC + lane * N;
-#pragma unroll
-        for (int j = 0; j < N; j += 4) y[k][j / 4] = *(const f32x4 *)(src + j);
-      }
-#pragma unroll
-      for (uint32_t k = 0; k < kAtOnce; ++k) {
-        const float gk = __shfl(g, (int)min(k0 + k, n - 1));
-        if (k0 + k >= n || !(there >> (k0 + k) & 1)) continue;
-#pragma unroll
-        for (int j = 0; j < N; ++j) acc[j] = __builtin_fmaf(y[k][j / 4][j % 4], gk, acc[j]);
-      }
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(part[k][e], fk, acc[e]);
     }
   }
+  if (i >= c.rows) return;
+  const uint32_t r = c.r0 + i, tok = a.by_heads.div(r), head = r - tok * a.heads;
   const float f = l > 0 ? 1.0f / l : l == 0 ? 0.0f : NAN;
-  Value *out = (Value *)a.out + (int64_t)(c.first + (int32_t)tok) * a.out_row + (int64_t)head * a.out_head + lane * N;
-  Value y[N] __attribute__((aligned(16)));
+  Value *out = (Value *)a.out + (int64_t)(c.first + (int32_t)tok) * a.out_row + (int64_t)head * a.out_head + half * (DC / 2) + 32 * b + 8 * g + 4 * h;
+  Value y[4] __attribute__((aligned(8)));
 #pragma unroll
-  for (int j = 0; j < N; ++j) y[j] = (Value)(acc[j] * f);
+  for (int e = 0; e < 4; ++e) y[e] = (Value)(acc[e] * f);
   if (a.out_vec) {
-#pragma unroll
-    for (int j = 0; j < N; j += 4) *(u32x2 *)(out + j) = *(u32x2 *)(y + j);
+    *(u32x2 *)out = *(u32x2 *)y;
   } else {
 #pragma unroll
-    for (int j = 0; j < N; ++j) out[j] = y[j];
+    for (int e = 0; e < 4; ++e) out[e] = y[e];
   }
-  if (lane == 0 && a.lse) a.lse[(size_t)(c.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+  if (blockIdx.y % (2 * kBlocks) == 0 && g == 0 && h == 0 && a.lse)
+    a.lse[(size_t)(c.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 
 }  // namespace uzip_kv

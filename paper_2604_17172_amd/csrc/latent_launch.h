@@ -15,15 +15,19 @@ static uzip_status launch(LatentCall &c) {
   const auto kernel = latent_kernel<T, CODE, LATENT_DIM, RG>;
   a.by_heads = FastDiv::of(a.heads);
   a.growth = (double)L::kRows / ((double)kTile * a.heads);
+  // What a block's beginning and end cost a workgroup, in tiles.  Counted as 1, workgroups with the end of one block and the
+  // beginning of the next were 30 % later than others.  Of 512: 6 (64 requests of up to 8190 tokens, 16 heads: 41 us, with 4
+  // 44, with 1 50); of 256: 4 (16 requests' pieces: 71 us, with 6 74, with 1 74).
+  a.begin = LATENT_DIM == 512 ? 6 : 4;
   // At most how much work there is: blocks, and the tiles of each.
   const uint64_t rows = (uint64_t)a.n_rows * a.heads;
   const uint64_t blocks = std::min<uint64_t>(rows / L::kRows + a.n_reqs + 1, (uint64_t)a.n_rows * ((a.heads + L::kRows - 1) / L::kRows));
   const uint64_t tiles = (((uint64_t)a.max_pages << a.page_shift) + kTile - 1) / kTile;
-  a.groups = (uint32_t)std::min<uint64_t>(c.units, std::max<uint64_t>(1, (blocks * (tiles + 1) + L::kMin - 1) / L::kMin));
+  a.groups = (uint32_t)std::min<uint64_t>(c.units, std::max<uint64_t>(1, (blocks * (tiles + a.begin) + 2 * a.begin - 1) / (2 * a.begin)));
   if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(typename L::Lds)) != hipSuccess) return UZIP_EHIP;
   kernel<<<a.groups, L::kThreads, sizeof(typename L::Lds), c.stream>>>(a);
   if (a.groups > 1)
-    latent_join_kernel<T, LATENT_DIM, L::kRows><<<dim3(a.groups - 1, L::kRows / 4), 256, 0, c.stream>>>(a);
+    latent_join_kernel<T, LATENT_DIM, RG><<<dim3(a.groups - 1, RG * 2 * L::kBlocks), 256, 0, c.stream>>>(a);
   return hipGetLastError() == hipSuccess ? UZIP_OK : UZIP_EHIP;
 }
 
