@@ -825,7 +825,7 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
   // the piece of workgroup w: the second of its slots where the block begins within its share
   auto slot_of = [&](uint32_t w) { return 2 * (size_t)w + (w == c.from ? 1 : 0); };
   auto ml_of = [&](uint32_t w) { return *(const f32x2 *)(a.part_ml + 2 * (slot_of(w) * kRows + i)); };
-  constexpr uint32_t kAtOnce = 8;  // pieces that are read side by side
+  constexpr uint32_t kAtOnce = 4;  // pieces that are read side by side
   float m = -INFINITY, l = 0;
   f32x4 acc = {0, 0, 0, 0};
   for (uint32_t w0 = c.from; w0 <= c.last; w0 += kAtOnce) {

@@ -226,6 +226,16 @@ def test_attend_many_requests(uz):
     attend_case(uz, 16, 256, 32, 2, "bf16", "e4m3fn", ctx, g.integers(0, 3, 300).tolist(), most=2)
 
 
+@pytest.mark.parametrize("n", [15, 16, 17, 33, 48, 63, 64, 65, 130])
+def test_attend_shares_of_so_many_requests(uz, n):
+    """The work before a request is summed over lanes, several requests to one from 64 on."""
+    g = np.random.default_rng(n)
+    ctx = (g.integers(0, 2, n) * g.integers(0, 1500, n)).tolist()
+    new = g.integers(0, 3, n).tolist()
+    new[n // 2] = 40
+    attend_case(uz, 16, 256, 32, 5, "bf16", "e4m3fn", ctx, new)
+
+
 @pytest.mark.parametrize("most", [0, 1, 7, 1 << 20])
 def test_attend_whatever_max_new_says(uz, most):
     attend_case(uz, 64, 512, 64, 12, "bf16", "e4m3fn", [100, 5, 700], [5, 9, 1], most=most)
@@ -390,6 +400,58 @@ def test_expanded(uz, case):
         out = got[0]
         base = torch.as_strided(out, (*out.shape[:2], out.shape[2] + 3), out.stride(), out.storage_offset() - 1)
         assert (base[:, :, 0] == 7).all() and (base[:, :, -2:] == 7).all()
+
+
+# Heads so many that a workgroup takes 64 rows of one ((rows / 32 + requests + 1) heads above 320), or 128 (of 64 rows: above 560).
+MANY_HEADS = [  # nope, rot, value, heads, kind, ctx, new, more
+    (128, 64, 128, 60, "bf16", [0], [200], {}),
+    (128, 64, 128, 150, "bf16", [0], [200], {}),
+    (128, 32, 128, 70, "fp16", [300, 0], [65, 64], dict(how="joined")),
+    (128, 64, 64, 130, "fp16", [0, 95, 31], [129, 1, 63], dict(how="fused")),
+    (64, 32, 64, 150, "bf16", [700], [130], {}),
+    (64, 32, 64, 61, "fp16", [250, 0], [127, 33], dict(how="joined")),
+    (64, 64, 128, 140, "bf16", [40], [160], dict(pad=5)),
+    (64, 32, 128, 66, "bf16", [128, 127, 129], [33, 34, 1], dict(pad=2)),
+    (128, 32, 64, 140, "bf16", [5], [150], dict(scale=-1.0)),
+    (128, 64, 128, 64, "bf16", [33], [190], dict(scale=0.0)),
+    (64, 64, 64, 150, "fp16", [64], [140], dict(scale=3.0)),
+    (64, 64, 64, 64, "bf16", [0], [180], dict(most=64)),
+    (128, 64, 128, 140, "fp16", [500, 2], [60, 60], dict(most=60)),
+]
+
+
+@pytest.mark.parametrize("case", MANY_HEADS, ids=str)
+def test_expanded_of_many_heads(uz, case):
+    *args, more = case
+    say("expanded", case)
+    expanded_case(uz, *args, **more)
+
+
+@pytest.mark.parametrize("heads", [64, 150])
+@pytest.mark.parametrize("nope,rot,value,kind", [(128, 64, 128, "bf16"), (64, 32, 64, "fp16"), (64, 64, 128, "bf16")])
+def test_expanded_of_many_heads_with_values_that_are_not_finite(uz, nope, rot, value, kind, heads):
+    """As if the tokens were not there, but for the rows and channels that see them."""
+    inf = float("inf")
+
+    def edit(q, k, r, v):
+        v[70, 3, 5], v[100, 3, 6], v[149, 9, 40] = float("nan"), inf, -inf
+        k[120, 7, 11] = float("nan")
+    *_, want, (out, lse) = expanded_case(uz, nope, rot, value, heads, kind, [10], [140], edit=edit)
+    at = 10 + np.arange(140)
+    odd = np.zeros(out.shape, bool)
+    odd[at >= 70, 3, 5] = odd[at >= 100, 3, 6] = odd[at >= 149, 9, 40] = odd[at >= 120, 7] = True
+    assert torch.isnan(out[torch.from_numpy(at >= 70), 3, 5]).all() and (out[torch.from_numpy(at >= 100), 3, 6] == inf).all()
+    assert (out[torch.from_numpy(at >= 149), 9, 40] == -inf).all() and torch.isnan(out[torch.from_numpy(at >= 120), 7]).all()
+    assert torch.isnan(lse[torch.from_numpy(at >= 120), 7]).all()
+    gone = torch.from_numpy(odd).cuda()
+    plain = {k: v.copy() if isinstance(v, np.ndarray) else v for k, v in want.items()}
+    for name in ("out", "spread", "floor"):
+        plain[name] = np.where(odd, 0.0, np.broadcast_to(plain[name], odd.shape) if np.ndim(plain[name]) else plain[name])
+    whole = odd.all(axis=2)
+    plain["lse"] = np.where(whole, 0.0, plain["lse"])
+    plain["size"] = np.where(whole, 0.0, np.broadcast_to(plain["size"], whole.shape))
+    check_attend((torch.where(gone, torch.zeros_like(out), out), torch.where(torch.from_numpy(whole).cuda(), torch.zeros_like(lse), lse)), plain, kind,
+                 nope + rot, 150, U_EXPANDED[kind], FLOOR_EXPANDED[kind])
 
 
 def test_expanded_many_requests(uz):
