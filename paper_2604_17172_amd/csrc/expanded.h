@@ -5,7 +5,7 @@
 // in one pass over the tokens with a running maximum.  A wave has a SIMD to itself and takes 64 rows (or 32),
 // so that what it reads from LDS serves two products: with 32 rows and two waves a SIMD, LDS was the bound.
 // In a round the weights of one tile of 32 tokens are worked out beside the scores of the next.  16 heads of 4096
-// tokens, causal, 128 + 64 and 128 channels in bf16: 118 us, 730 TFLOP/s of 86 GFLOP.  A round takes 2500 cycles, of which
+// tokens, causal, 128 + 64 and 128 channels in bf16: 114 us, 750 TFLOP/s of 86 GFLOP.  A round takes 2500 cycles, of which
 // the matrix unit works 1280: a wave issues 345 instructions and 32 exponentials in it.  A workgroup's
 // begin and end take 12 us, of which there are two on each compute unit.
 #pragma once

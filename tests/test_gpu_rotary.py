@@ -88,6 +88,10 @@ CASES = [  # rows, heads, dim, rot, first, interleaved, how
     (1025, 4, 576, 64, 512, False, ""),
     (7, 2, 24, 16, 8, True, "fused"),
     (9, 3, 40, 32, 8, False, ""),
+    (50, 3, 44, 24, 4, False, ""),
+    (61, 3, 44, 24, 4, True, "fused"),
+    (700, 5, 104, 40, 64, True, ""),
+    (3, 2, 30, 12, 2, False, ""),
 ]
 
 
