@@ -80,7 +80,8 @@ uzip_status uzip_latent_attend(const uzip_latent_cache *cache, uzip_dtype dtype,
  * nope and value are 64 or 128, rot 32 or 64; dtype is UZIP_BF16 or UZIP_FP16.  Scores and sums are
  * held in 32 bits; weights enter the second product in dtype.  A row that sees nothing gives zeros
  * and -infinity.  A value that is infinite or NaN reaches the rows that see it, and no others.
- *   max_new:  the most new tokens of a request: it chooses kernels, a wrong value costs time.
+ *   max_new:  the most new tokens of a request: it chooses kernels, a wrong value costs
+ *             time and the last bits may differ.
  *   d_lse:    [n_rows][n_heads] (may be NULL).
  * Errors: EINVAL, EHIP, EUNSUPPORTED. */
 uzip_status uzip_latent_attend_expanded(uzip_dtype dtype, const void *d_q, int64_t q_row, int64_t q_head, uint32_t n_rows,

@@ -229,6 +229,7 @@ __global__ __launch_bounds__(256, 1) void expanded_kernel(ExpandedArgs a) {
   f32x16 acc[R][kBlocks], s[2][R];  // scores of this round's tile and of the next
   u32x4 w[R][2];
   float m[R], l[R], most[R], ref[R];
+  float lift = 0;  // weights are 2^-lift times as large
   // `count` steps, each with a read from LDS: two are on their way while the two before them are used, and
   // beside(i) is what the vector units do meanwhile.  The order is the one written here: the wave has its SIMD for
   // itself, and only what stands beside a matrix instruction runs beside it.
@@ -288,7 +289,7 @@ __global__ __launch_bounds__(256, 1) void expanded_kernel(ExpandedArgs a) {
         const float both = max_of_halves(most[r]);
         const float next = both > m[r] + kLag ? both : m[r], f = next == m[r] ? 1.0f : __builtin_amdgcn_exp2f(m[r] - next);
         m[r] = next;
-        ref[r] = next == -INFINITY ? 0.0f : next;
+        ref[r] = next == -INFINITY ? 0.0f : next + lift;
         l[r] *= f;
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n)
@@ -450,6 +451,7 @@ __global__ __launch_bounds__(256, 1) void expanded_kernel(ExpandedArgs a) {
     if (!notes.trouble) break;
     __syncthreads();
     careful = true;
+    if (T == UZIP_BF16) lift = 32;  // sums of values near the type's largest stay finite
     ask_first();
   }
 
@@ -469,6 +471,7 @@ __global__ __launch_bounds__(256, 1) void expanded_kernel(ExpandedArgs a) {
   for (int r = 0; r < R; ++r) {
     const uint32_t j = 32 * (R * rg + r) + col;
     l[r] = sum_of_halves(l[r]);
+    m[r] += lift;
     if (h == 0) {
       join.m[group][j] = m[r];
       join.l[group][j] = l[r];
@@ -493,8 +496,11 @@ __global__ __launch_bounds__(256, 1) void expanded_kernel(ExpandedArgs a) {
       sum = __builtin_fmaf(join.l[g][j], scale[g], sum);
     }
     if ((int32_t)j >= b.rows) continue;
-    const float f = m[r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[r] - all);
+    // divided before they are added: a group's sums may be finite and all of them together not
     const float inverse = sum > 0 ? 1.0f / sum : sum == 0 ? 0.0f : NAN;
+    const float f = m[r] == -INFINITY ? 0.0f * inverse : __builtin_amdgcn_exp2f(m[r] - all) * inverse;
+#pragma unroll
+    for (int g = 0; g < SPLIT; ++g) scale[g] *= inverse;
     Value *out = (Value *)a.out + (int64_t)(b.first + (int32_t)j) * a.out_row + (int64_t)head * a.out_head;
 #pragma unroll
     for (int n = 0; n < kBlocks; ++n) {
@@ -515,7 +521,7 @@ __global__ __launch_bounds__(256, 1) void expanded_kernel(ExpandedArgs a) {
         Value y[4] __attribute__((aligned(8)));
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          float z = x[k] * inverse;
+          float z = x[k];
           if (careful) {
             if (at[r] >= notes.first_of[0][d + k]) z = NAN;
             if (at[r] >= notes.first_of[1][d + k]) z += INFINITY;

@@ -454,6 +454,15 @@ def test_expanded_of_many_heads_with_values_that_are_not_finite(uz, nope, rot, v
                  nope + rot, 150, U_EXPANDED[kind], FLOOR_EXPANDED[kind])
 
 
+@pytest.mark.parametrize("heads", [2, 64, 150])
+def test_expanded_values_near_the_largest(uz, heads):
+    """Sums of values that 32 bits hold one by one, but not added up: divided first, they are within the type."""
+    def edit(q, k, r, v):
+        v.mul_(2.0 ** 126 / v.abs().max())
+    *_, want, (out, lse) = expanded_case(uz, 128, 64, 128, heads, "bf16", [60], [140], edit=edit)
+    check_attend((out, lse), want, "bf16", 192, 200, U_EXPANDED["bf16"], FLOOR_EXPANDED["bf16"])
+
+
 def test_expanded_many_requests(uz):
     expanded_case(uz, 64, 32, 64, 1, "bf16", [0] * 150, [1, 2, 0] * 50)
 
