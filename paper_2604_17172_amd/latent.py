@@ -15,7 +15,7 @@ import torch
 
 from . import BF16, EINVAL, FP16, OK, _check, _dev_empty, _lib
 from .kv import _CODES, _TYPES, _device, _handle, _i64, _int, _ints, _need, _on, _rows, _sz, _u32, _vp, _f32
-from .rotary import _queries, _query_args, _turn, _turn_p
+from .rotary import _queries, _query_args, _serves, _turn, _turn_p
 
 _c = ctypes
 
@@ -80,13 +80,6 @@ def _current(cache: LatentCache) -> int:
     if cache.index != device:
         raise ValueError("the cache is on another GPU than the current one")
     return device
-
-
-def _serves(*tensors) -> None:
-    if torch.is_grad_enabled():
-        for x in tensors:
-            if x is not None and x.requires_grad:
-                raise ValueError("no gradient goes through this call: detach its inputs, or call it under torch.no_grad()")
 
 
 def _vectors(x: torch.Tensor, name: str, dim: int, device: int) -> int:

@@ -157,6 +157,13 @@ def rotate(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, interle
     return _rotate(x, positions, freq, interleaved, first, magnitude, inverse, out, stream)
 
 
+def _serves(*tensors) -> None:
+    if torch.is_grad_enabled():
+        for x in tensors:
+            if x is not None and x.requires_grad:
+                raise ValueError("no gradient goes through this call: detach its inputs, or call it under torch.no_grad()")
+
+
 def _queries(q, q_out, rows: int, dim: int, device: int, kind: int, stream):
     """(x, out) of the queries that are turned beside a store, or (None, None)."""
     if q is None:
@@ -183,8 +190,9 @@ def kv_rotate_store(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions:
                     runs: torch.Tensor, counts: torch.Tensor, q: torch.Tensor | None = None, interleaved: bool = False, first: int = 0,
                     magnitude: float = 1.0, q_out: torch.Tensor | None = None, stream=None):
     """kv_store with the keys turned on the way (their codes are the only rounding), and the step's queries
-    q [rows, query heads, dim] turned in the same launch.  Returns q_out, None without q."""
+    q [rows, query heads, dim] turned in the same launch.  No gradient goes through it.  Returns q_out, None without q."""
     device = _current(cache)
+    _serves(k, v, q, q_out)
     t = _rows(k, "k", cache.dim, device)
     if _rows(v, "v", cache.dim, device) != t or k.shape != v.shape or k.shape[1] != cache.heads:
         raise ValueError("k and v are [rows, the cache's heads, dim] of one type")

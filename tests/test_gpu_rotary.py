@@ -344,7 +344,9 @@ def test_refusals(uz):
     slots, runs, counts = torch.zeros(4, dtype=torch.int64, device="cuda"), ints([[0, 1]]), ints([0, 0])
     k = torch.zeros(4, 2, 64, dtype=torch.bfloat16, device="cuda")
     for b in [dict(k=k[:, :1]), dict(q=k[:2]), dict(q=k.float()), dict(q_out=k), dict(q=k, q_out=k[:, :1]), dict(f=dev(freq_of(66))), dict(first=1),
-              dict(slots=slots[:2])]:
+              dict(slots=slots[:2]), dict(q=k.clone().requires_grad_(True)), dict(k=k.clone().requires_grad_(True))]:
         a = {"k": k, "q": None, "q_out": None, "f": f, "first": 0, "slots": slots, **b}
         with pytest.raises(ValueError):
             uz.kv_rotate_store(cache, a["k"], k, p, a["f"], a["slots"], runs, counts, q=a["q"], q_out=a["q_out"], first=a["first"])
+    with torch.no_grad():                                                 # what a server's call looks like
+        uz.kv_rotate_store(cache, k, k, p, f, slots, runs, counts, q=k.clone().requires_grad_(True))
