@@ -97,7 +97,7 @@ __device__ __forceinline__ bool find_expanded(const ExpandedArgs &a, uint32_t in
   return true;
 }
 
-// Four waves of R times 32 rows: RG side by side share their tiles of 32 tokens, and SPLIT such groups take
+// Four or eight waves of R times 32 rows: RG side by side share their tiles of 32 tokens, and SPLIT such groups take
 // the tiles in turn; their sums are joined at the end.
 template <int DN, int DR, int DV, int R, int RG, int SPLIT>
 struct Expanded {
@@ -119,11 +119,11 @@ struct Expanded {
     Tile tile[kPlaces][SPLIT];
     Join join;
   };
-  static_assert(kWaves == 4 && sizeof(Lds) <= kMemory && sizeof(Join) + sizeof(Notes) <= sizeof(Lds), "the tiles' memory holds the rest");
+  static_assert((kWaves == 4 || kWaves == 8) && sizeof(Lds) <= kMemory && sizeof(Join) + sizeof(Notes) <= sizeof(Lds), "the tiles' memory holds the rest");
 };
 
 template <int T, int DN, int DR, int DV, int R, int RG, int SPLIT, bool DIRECT>
-__global__ __launch_bounds__(256, 1) void expanded_kernel(ExpandedArgs a) {
+__global__ __launch_bounds__(64 * RG * SPLIT, RG * SPLIT / 4) void expanded_kernel(ExpandedArgs a) {
   typedef Expanded<DN, DR, DV, R, RG, SPLIT> L;
   typedef typename Elem<T>::type Value;
   typedef typename LatentType<T>::Eight Eight;
@@ -358,6 +358,7 @@ __global__ __launch_bounds__(256, 1) void expanded_kernel(ExpandedArgs a) {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) query[r][s] = __builtin_bit_cast(Eight, __builtin_bit_cast(s16x8, query[r][s]) ^ (short)0x8000);
   }
+  if constexpr (L::kWaves == 4)  // half of the registers
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll

@@ -35,12 +35,12 @@ uzip_status uzip_latent_attend_expanded(uzip_dtype dtype, const void *d_q, int64
   c.type = dtype;
   c.rot = rot;
   c.value = value;
-  // Rows of a workgroup.  Four waves take 128 rows (two by two, each pair half of the tokens), or 64 or 32 rows (each wave a
-  // quarter of the tokens): fewer where that leaves compute units idle.  In bf16, 128 + 64 and 128 channels, us with
+  // Rows of a workgroup.  Four waves take 128 rows (two by two, each pair half of the tokens; or eight waves, a quarter each), or
+  // 64 or 32 rows (each wave a quarter of the tokens): fewer where that leaves compute units idle.  In bf16, 128 + 64 and 128 channels, us with
   // 128, 64, 32 rows: 1024 tokens of 8 heads 29, 21, 16; 2048 of 16 heads 49, 44, 63; 4 x 1024 of 16 heads 54, 66, 94;
   // 8 x 512 of 8 heads 24, 33, 42; 32 x 64 behind 1000 of 16 heads 77, 74, 103; 64 x 30 behind 1000 of 8 heads 71, 70, 67.
   auto blocks = [&](uint32_t rows) { return ((uint64_t)n_rows / rows + n_reqs + 1) * n_heads; };
-  c.rows = max_new <= 32 || blocks(32) <= 320 ? 32 : max_new <= 64 || blocks(64) <= 560 ? 64 : 128;
+  c.rows = max_new <= 32 || blocks(32) <= 320 ? 32 : max_new <= 64 || blocks(64) <= (expanded_by_eight(nope, rot, value) ? 512 : 560) ? 64 : 128;
   c.stream = stream;
   return nope == 64 ? launch_expanded<64>(c) : launch_expanded<128>(c);
 }

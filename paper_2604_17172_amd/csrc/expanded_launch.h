@@ -19,7 +19,8 @@ static uzip_status launch(const ExpandedCall &c) {
 template <int T, int DR, int DV>
 static uzip_status launch(const ExpandedCall &c) {
   if (!c.direct) return launch<T, DR, DV, 1, 1, 4, false>(c);
-  return c.rows == 32 ? launch<T, DR, DV, 1, 1, 4, true>(c) : c.rows == 64 ? launch<T, DR, DV, 2, 1, 4, true>(c) : launch<T, DR, DV, 2, 2, 2, true>(c);
+  return c.rows == 32 ? launch<T, DR, DV, 1, 1, 4, true>(c) : c.rows == 64 ? launch<T, DR, DV, 2, 1, 4, true>(c)
+                                                                         : launch<T, DR, DV, 2, 2, expanded_by_eight(EXPANDED_NOPE, DR, DV) ? 4 : 2, true>(c);
 }
 template <int T>
 static uzip_status launch(const ExpandedCall &c) {
