@@ -76,13 +76,14 @@ def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", f
 def _turn(positions: torch.Tensor, freq: torch.Tensor, rows: int, device: int, interleaved: bool, first: int, magnitude: float,
           inverse: bool) -> uzip_turn:
     _ints(positions, "positions", device)
-    if freq.get_device() != device or freq.dtype != torch.float32 or freq.dim() != 1 or not freq.is_contiguous():
+    if freq.get_device() != device or freq.dtype is not torch.float32 or freq.dim() != 1 or not freq.is_contiguous():
         raise ValueError("freq is a contiguous fp32 vector on the current GPU")
     if positions.numel() < rows:
         raise ValueError("positions has an entry for each row")
-    if not 0 <= first <= 1024 or not 1 <= freq.numel() <= 512:
+    half = freq.numel()
+    if not 0 <= first <= 1024 or not 1 <= half <= 512:
         raise ValueError("the rotary part is 2 to 1024 channels from first on")
-    return uzip_turn(positions.data_ptr(), freq.data_ptr(), 2 * freq.numel(), first, bool(interleaved), bool(inverse), magnitude)
+    return uzip_turn(positions.data_ptr(), freq.data_ptr(), 2 * half, first, bool(interleaved), bool(inverse), magnitude)
 
 
 def kv_positions(lens: torch.Tensor, q_start: torch.Tensor, rows: int, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
@@ -183,7 +184,8 @@ def _queries(q, q_out, rows: int, dim: int, device: int, kind: int, stream):
 def _query_args(q, q_out):
     if q is None:
         return None, 0, 0, 0, None, 0, 0
-    return q.data_ptr(), q.stride(0), q.stride(1), q.shape[1], q_out.data_ptr(), q_out.stride(0), q_out.stride(1)
+    step, out_step = q.stride(), q_out.stride()
+    return q.data_ptr(), step[0], step[1], q.shape[1], q_out.data_ptr(), out_step[0], out_step[1]
 
 
 def kv_rotate_store(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, slots: torch.Tensor,
@@ -194,20 +196,22 @@ def kv_rotate_store(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions:
     device = _current(cache)
     _serves(k, v, q, q_out)
     t = _rows(k, "k", cache.dim, device)
-    if _rows(v, "v", cache.dim, device) != t or k.shape != v.shape or k.shape[1] != cache.heads:
+    shape = k.shape
+    if _rows(v, "v", cache.dim, device) != t or v.shape != shape or shape[1] != cache.heads:
         raise ValueError("k and v are [rows, the cache's heads, dim] of one type")
     _ints(slots, "slots", device, torch.int64)
     _ints(runs, "runs", device)
     _ints(counts, "counts", device)
-    rows = k.shape[0]
-    if slots.numel() < rows or counts.numel() < 2 or runs.numel() != 2 * runs.shape[0]:
+    rows, n_runs = shape[0], runs.shape[0]
+    if slots.numel() < rows or counts.numel() < 2 or runs.numel() != 2 * n_runs:
         raise ValueError("slots has an entry for each row, runs two for each run, counts two")
     turn = _turn(positions, freq, rows, device, interleaved, first, magnitude, False)
     if first + turn.rot > cache.dim:
         raise ValueError("the rotary part lies within dim")
     q, q_out = _queries(q, q_out, rows, cache.dim, device, t, stream)
-    rc = uzip_kv_rotate_store(cache, t, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), rows,
-                              slots.data_ptr(), runs.data_ptr(), counts.data_ptr(), runs.shape[0], _c.byref(turn), *_query_args(q, q_out),
+    k_step, v_step = k.stride(), v.stride()
+    rc = uzip_kv_rotate_store(cache, t, k.data_ptr(), k_step[0], k_step[1], v.data_ptr(), v_step[0], v_step[1], rows,
+                              slots.data_ptr(), runs.data_ptr(), counts.data_ptr(), n_runs, _c.byref(turn), *_query_args(q, q_out),
                               _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_kv_rotate_store")
