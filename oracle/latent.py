@@ -32,10 +32,11 @@ def _row(z, values):
 def attend(q, codes, exps, latent: int, fmt: str, table, lens, q_start, page: int, scale: float) -> dict:
     """Besides out and lse: `spread`, the sum of p |c| for each output, `size`, the largest scale * sum |q k| of a
     row, and `floor`, the sum of |code_t| over sum_t 2^(g_t - max g - e_t) with g_t = s_t log2(e) + e_t: what an error of 1 of a
-    weight 2^(g_t - max g) on every token would make of an output."""
+    weight 2^(g_t - max g) on every token would make of an output; `tiles`, the same of an error of 1 relative to the largest
+    weight of 64 tokens that begin at a multiple of 64."""
     q = np.asarray(q, dtype=np.float64)
     rows, heads, _ = q.shape
-    out, spread, floor = (np.zeros((rows, heads, latent)) for _ in range(3))
+    out, spread, floor, tiles = (np.zeros((rows, heads, latent)) for _ in range(4))
     lse, size, shift = np.full((rows, heads), -np.inf), np.zeros((rows, heads)), np.zeros((rows, heads))
     values = code_values(fmt)
     for i in range(len(lens)):
@@ -60,8 +61,11 @@ def attend(q, codes, exps, latent: int, fmt: str, table, lens, q_start, page: in
             g = z * np.log2(np.e) + e[:n, 0]
             under = (2.0 ** (g - g.max(axis=1, keepdims=True) - e[:n, 0])).sum(axis=1)
             floor[r] = np.abs(raw[:n, :latent]).sum(axis=0) / under[:, None]
+            starts = np.flatnonzero(np.diff(t[:n] // 64, prepend=-1))
+            most = 2.0 ** (np.maximum.reduceat(g, starts, axis=1) - g.max(axis=1, keepdims=True))
+            tiles[r] = most @ np.add.reduceat(np.abs(raw[:n, :latent]), starts, axis=0) / under[:, None]
             shift[r] = np.abs(e[:n, 0]).max()
-    return {"out": out, "lse": lse, "spread": spread, "size": size, "floor": floor, "shift": shift}
+    return {"out": out, "lse": lse, "spread": spread, "size": size, "floor": floor, "tiles": tiles, "shift": shift}
 
 
 def expanded(q, k, key_rot, v, q_start, k_start, scale: float) -> dict:

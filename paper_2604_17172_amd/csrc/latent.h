@@ -10,7 +10,9 @@
 //
 // A token's scale 2^e belongs to its weight in the second product: with
 //   g_t = s_t log2(e) + e_t,  w_t = 2^(g_t - m),  acc = sum w_t code_t,  l = sum w_t 2^-e_t
-// out = acc / l, and the running maximum m is taken over g.
+// out = acc / l, and the running maximum m is taken over g.  The weights of a tile count from the tile's own largest, 2^k of
+// them from m as the matrix instruction's scale: of eight bits each, counted from m a long tail of small weights would end up as nothing
+// beside one large one.  l holds its exponent apart, for the 2^-e_t of a row may lie 2^219 from one another.
 #pragma once
 
 #include <type_traits>
@@ -39,7 +41,7 @@ struct LatentArgs {
   int64_t q_row, q_head, out_row, out_head;
   const int32_t *table, *lens, *q_start;
   float *part_acc;  // [slot][32 rows][channels' half][32 channels][8 of them][lane][4]
-  float *part_ml;   // [slot][row][2]
+  float *part_ml;   // [slot][row][4]: the power of two that the sums count from, l, l's power of two, none
   struct LatentCut *cuts;  // of each workgroup
   uint32_t n_pages, page_shift, rot;
   uint32_t n_rows, heads, max_pages, n_reqs;
@@ -53,6 +55,9 @@ struct LatentArgs {
 
 constexpr int kTile = 64;  // tokens
 constexpr int kAhead = 4;  // reads of the first product under way
+// Sums of weights times codes are 2^-15 of what they stand for, so that the factor that makes them an output is a number of 32 bits
+// wherever latents are: 2^(15 - 7) times a token's scale of up to 2^119, or a 2^29-th of 2^(15 - 7 - 4) times 2^-100.
+constexpr int kDown = 15;
 // ------------------------------------------------------------------ pieces of work
 struct LatentRequest {
   int32_t first, rows, len, base;  // first row of the step's arrays, new tokens, tokens, place of the first new one
@@ -328,6 +333,27 @@ __device__ __forceinline__ float sum_of_halves(float x) {
 __device__ __forceinline__ void load_to_lds(const uint8_t *base, uint32_t offset, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(uniform(to)), "v"(offset), "s"(uniform((uint64_t)(uintptr_t)base)) : "memory");
 }
+// x 2^by; by may be infinite, or what is left of one infinity less another: then x is nothing.
+__device__ __forceinline__ float times_pow2(float x, float by) { return __builtin_ldexpf(x, (int)__builtin_amdgcn_fmed3f(by, -500.0f, 500.0f)); }
+// A sum and the power of two that it counts from, at first from none.
+struct Sum {
+  float x = 0, unit = -INFINITY;
+  // where the sum stays in [1/2, 2^100), the unit stays; for sums of a wave's lanes
+  __device__ __forceinline__ void add(float y, float y_unit) {
+    const float next = x + times_pow2(y, y_unit - unit);
+    if (__any(!(next < 0x1p100f))) {
+      const float to = fmaxf(unit, y == 0 ? -INFINITY : y_unit + (float)__builtin_amdgcn_frexp_expf(y));
+      x = times_pow2(x, unit - to) + times_pow2(y, y_unit - to);
+      unit = to;
+    } else {
+      x = next;
+    }
+  }
+  __device__ __forceinline__ void rebase(float to) {
+    x = times_pow2(x, unit - to);
+    unit = to;
+  }
+};
 // x, from which nothing is computed before this place: what only a seldom taken branch needs would else be
 // kept in registers through the loop around it.
 __device__ __forceinline__ uint32_t only_here(uint32_t x) {
@@ -356,14 +382,16 @@ template <int T, int CODE, int DC, int RG>
 struct Latent {
   static constexpr int kRows = 32 * RG, kThreads = 256 * RG, kBlocks = DC / 64, kSteps = DC / 32;
   static constexpr int kBufs = 3;      // tiles in LDS: one whose values are read, one whose keys are, one under way
-  static constexpr float kLag = 5;     // weights up to 2^5: times 2^3 they are codes
+  static constexpr float kTop = 7;     // a tile's largest weight is a code of 2^7 up to 2^8; less only where scores are past 2^24
+  static constexpr float kLag = 4;     // how far a tile's may pass the reference of the sums
   typedef LatentTile<DC> Tile;
   struct Lds {
     Tile tile[kBufs];
     i32x4 weights[2][RG][2][LatentType<T>::kTerms][64];  // of two rounds: a half's tokens, as the lanes scored them
-    float factor[2][RG][32];                             // on the sums before them
+    f32x2 factor[2][RG][32];                             // on the sums before them; the weights' scale byte
     float most[RG][2][32];
-    float m[RG][32], l[RG][2][32];
+    float m[RG][32];
+    f32x2 l[RG][2][32];                                  // and its power of two
     uint32_t trouble;
     int32_t first_bad;
   };
@@ -478,10 +506,11 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
         // token col of this wave's half, chunk 2 k + h
         const uint32_t k_off = (32 * half + col) * DC + ((h ^ swizzle(col & 15)) << 4);
         const uint32_t r_off = (uint32_t)offsetof(Tile, rot) + (32 * half + col) * 64 + ((h ^ ((col >> 2) & 3)) << 4);
-        float m = -INFINITY, l = 0;
+        float m = -INFINITY;  // a power of two, as are the tiles'
+        Sum l;
 #pragma unroll
         for (int term = 0; term < TERMS; ++term) lds.weights[1][rg][half][term][lane] = i32x4{0, 0, 0, 0};  // before the first
-        lds.factor[1][rg][col] = 1;
+        lds.factor[1][rg][col] = f32x2{1, 0};
         for (uint32_t i = 0; i < rounds; ++i) {
           __syncthreads();  // tile i is there
           if (careful) __syncthreads();
@@ -537,25 +566,26 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
           if (h == 0) lds.most[rg][half][col] = most;
           __syncthreads();
 
-          // the reference of this tile's weights, the factor on the sums so far, the weights
+          // the reference of this tile's weights and of the sums, the factor on the sums so far, the weights
           f32x4 inv[4];
 #pragma unroll
           for (int g = 0; g < 4; ++g) inv[g] = *(LdsFloats)(uintptr_t)(of_four + offsetof(Tile, inv) + 32 * g);
           most = fmaxf(lds.most[rg][0][col], lds.most[rg][1][col]);
-          const float next = most > m + L::kLag ? most : m;
-          const float f = next == m ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+          const float ref = __builtin_floorf(most) - L::kTop;
+          const float next = ref > m + L::kLag ? ref : m;
+          if (half == 0 && h == 0)  // 2^(ref - m - kDown) as an exponent byte; what is below 2^-127 ends there
+            lds.factor[i & 1][rg][col] = f32x2{next == m ? 1.0f : times_pow2(1.0f, m - next), __int_as_float(127 - kDown + (int)fmaxf(ref - next, kDown - 127.0f))};
           m = next;
-          l *= f;
-          if (half == 0 && h == 0) lds.factor[i & 1][rg][col] = f;
-          const float ref = m == -INFINITY ? 0.0f : m - 3.0f;
+          const float from = ref == -INFINITY ? 0.0f : ref;
+          float sum = 0;
           i32x4 w[TERMS];
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             float y[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              y[k] = __builtin_amdgcn_exp2f(s[4 * g + k] - ref);  // 2^3 times the weight
-              l = __builtin_fmaf(y[k], inv[g][k], l);
+              y[k] = __builtin_amdgcn_exp2f(s[4 * g + k] - from);
+              sum = __builtin_fmaf(y[k], inv[g][k], sum);
             }
 #pragma unroll
             for (int term = 0; term < TERMS; ++term) {
@@ -573,15 +603,17 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
           }
 #pragma unroll
           for (int term = 0; term < TERMS; ++term) lds.weights[i & 1][rg][half][term][lane] = w[term];
+          l.add(sum, ref);
         }
         // the adding waves' last round
         __syncthreads();
-        l = sum_of_halves(l);
+        l.rebase(max_of_halves(l.unit));
+        l.x = sum_of_halves(l.x);
         if (h == 0) {
-          lds.l[rg][half][col] = l;
-          lds.m[rg][col] = m - 3.0f;  // what the weights' sums count from
+          lds.l[rg][half][col] = f32x2{l.x, l.unit};
+          lds.m[rg][col] = m;  // what the weights' sums count from
         }
-        if (__any(l * 0.0f != 0.0f) && lane == 0) lds.trouble = 1;
+        if (__any(l.x * 0.0f != 0.0f) && lane == 0) lds.trouble = 1;
         __syncthreads();
         again = !careful && lds.trouble != 0;
         __syncthreads();
@@ -715,7 +747,10 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
 
           // The products of tile i - 1; in the first round of tile 0 and weights that are 0.
           const uint32_t before = tiles0 + (i ? i - 1 : 0) % L::kBufs * (uint32_t)sizeof(Tile) + v_off;
-          const float f = lds.factor[(i + 1) & 1][rg][col];
+          const f32x2 factor = lds.factor[(i + 1) & 1][rg][col];
+          const float f = factor[0];
+          const int scale = __float_as_int(factor[1]);
+          constexpr int kTermScales = 0x777B7F;  // 2^0, 2^-4, 2^-8
           i32x8 w[TERMS], v[2];
 #pragma unroll
           for (int term = 0; term < TERMS; ++term) {
@@ -744,9 +779,10 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
 #pragma unroll
           for (int b = 0; b < L::kBlocks; ++b) {
             if (b + 1 < L::kBlocks) values(b + 1);
-#pragma unroll
-            for (int term = 0; term < TERMS; ++term)
-              acc[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v[b % 2], w[term], acc[b], CODE == UZIP_E4M3FN ? 0 : 1, 0, 0, 127, 0, 127 - 4 * term);
+            times<TERMS>([&](auto number) {
+              constexpr int term = decltype(number)::value;
+              acc[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v[b % 2], w[term], acc[b], CODE == UZIP_E4M3FN ? 0 : 1, 0, term, kTermScales, 0, scale);
+            });
             if (b == L::kBlocks / 2 - 1 && i < rounds) __syncthreads();
           }
         }
@@ -763,14 +799,15 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
         again = !careful && lds.trouble != 0;
         const uint32_t col = only_here(threadIdx.x & 31), h = only_here(threadIdx.x & 63) >> 5, r = r0 + 32 * rg + col;
         const uint32_t tok = a.by_heads.div(r), head = r - tok * a.heads;
-        float l = lds.l[rg][0][col] + lds.l[rg][1][col];
-        const float m = lds.m[rg][col];
+        const f32x2 l0 = lds.l[rg][0][col], l1 = lds.l[rg][1][col];
+        const float unit = fmaxf(l0[1], l1[1]), m = lds.m[rg][col];
+        float l = times_pow2(l0[0], l0[1] - unit) + times_pow2(l1[0], l1[1] - unit);
         if (careful && q.base + (int32_t)tok >= lds.first_bad) l = NAN;
         __syncthreads();
         if (!again && r < list) {
           const LatentArgs a = read_again();
           if (whole) {
-            const float f = l > 0 ? 1.0f / l : l == 0 ? 0.0f : NAN;
+            const float f = times_pow2(l > 0 ? 1.0f / l : l == 0 ? 0.0f : NAN, m - unit + kDown);
             Value *out = (Value *)a.out + (int64_t)(q.first + (int32_t)tok) * a.out_row + (int64_t)head * a.out_head + channel0;
 #pragma unroll
             for (int b = 0; b < L::kBlocks; ++b)
@@ -788,7 +825,7 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
                 }
               }
             if (half == 0 && h == 0 && a.lse)
-              a.lse[(size_t)(q.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+              a.lse[(size_t)(q.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (unit + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
           } else {
             const size_t slot = 2 * (size_t)blockIdx.x + (begin > place.before ? 0 : 1), row = slot * L::kRows + 32 * rg + col;
             f32x4 *part = (f32x4 *)a.part_acc + (((slot * RG + rg) * 2 + half) * L::kBlocks * 4) * 64 + 32 * h + col;  // as the lanes hold them
@@ -801,10 +838,7 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
                 for (int k = 0; k < 4; ++k) y[k] = acc[b][4 * g + k];
                 part[(4 * b + g) * 64] = y;
               }
-            if (half == 0 && h == 0) {
-              a.part_ml[2 * row] = m;
-              a.part_ml[2 * row + 1] = l;
-            }
+            if (half == 0 && h == 0) *(f32x4 *)(a.part_ml + 4 * row) = f32x4{m, l, unit, 0};
           }
         }
       }
@@ -828,12 +862,13 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
   if (!c.cut || 32 * rg >= c.rows) return;
   // the piece of workgroup w: the second of its slots where the block begins within its share
   auto slot_of = [&](uint32_t w) { return 2 * (size_t)w + (w == c.from ? 1 : 0); };
-  auto ml_of = [&](uint32_t w) { return *(const f32x2 *)(a.part_ml + 2 * (slot_of(w) * kRows + i)); };
+  auto ml_of = [&](uint32_t w) { return *(const f32x4 *)(a.part_ml + 4 * (slot_of(w) * kRows + i)); };
   constexpr uint32_t kAtOnce = 4;  // pieces that are read side by side
-  float m = -INFINITY, l = 0;
+  float m = -INFINITY;
+  Sum sum;
   f32x4 acc = {0, 0, 0, 0};
   for (uint32_t w0 = c.from; w0 <= c.last; w0 += kAtOnce) {
-    f32x2 ml[kAtOnce];
+    f32x4 ml[kAtOnce];
     f32x4 part[kAtOnce];
 #pragma unroll
     for (uint32_t k = 0; k < kAtOnce; ++k) {
@@ -844,23 +879,22 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
     float top = m;
 #pragma unroll
     for (uint32_t k = 0; k < kAtOnce; ++k) top = fmaxf(top, ml[k][0]);
-    const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-    l *= f;
+    const float f = m == top ? 1.0f : times_pow2(1.0f, m - top);
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] *= f;
     m = top;
 #pragma unroll
     for (uint32_t k = 0; k < kAtOnce; ++k) {
       if (w0 + k > c.last || ml[k][1] == 0) continue;  // a piece of no weight has no sums
-      const float fk = ml[k][0] == top ? 1.0f : __builtin_amdgcn_exp2f(ml[k][0] - top);
-      l = __builtin_fmaf(ml[k][1], fk, l);
+      const float fk = ml[k][0] == top ? 1.0f : times_pow2(1.0f, ml[k][0] - top);
+      sum.add(ml[k][1], ml[k][2]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(part[k][e], fk, acc[e]);
     }
   }
   if (i >= c.rows) return;
   const uint32_t r = c.r0 + i, tok = a.by_heads.div(r), head = r - tok * a.heads;
-  const float f = l > 0 ? 1.0f / l : l == 0 ? 0.0f : NAN;
+  const float l = sum.x, f = times_pow2(l > 0 ? 1.0f / l : l == 0 ? 0.0f : NAN, m - sum.unit + kDown);
   Value *out = (Value *)a.out + (int64_t)(c.first + (int32_t)tok) * a.out_row + (int64_t)head * a.out_head + half * (DC / 2) + 32 * b + 8 * g + 4 * h;
   Value y[4] __attribute__((aligned(8)));
 #pragma unroll
@@ -872,7 +906,7 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
     for (int e = 0; e < 4; ++e) out[e] = y[e];
   }
   if (blockIdx.y % (2 * kBlocks) == 0 && g == 0 && h == 0 && a.lse)
-    a.lse[(size_t)(c.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    a.lse[(size_t)(c.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (sum.unit + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 
 }  // namespace uzip_kv

@@ -159,7 +159,7 @@ uzip_status uzip_latent_store(const uzip_latent_cache *cache, uzip_dtype dtype, 
 
 size_t uzip_latent_attend_workspace(uint32_t latent, uint32_t n_rows, uint32_t n_heads, uint32_t n_reqs, uint32_t max_new) {
   if ((latent != 256 && latent != 512) || !attend_sizes(n_rows, n_heads, n_reqs)) return 0;
-  return (size_t)2 * kLatentUnits * latent_rows(n_rows, n_heads, max_new) * (latent + 2) * sizeof(float) + kLatentUnits * sizeof(LatentCut);
+  return (size_t)2 * kLatentUnits * latent_rows(n_rows, n_heads, max_new) * (latent + 4) * sizeof(float) + kLatentUnits * sizeof(LatentCut);
 }
 
 uzip_status uzip_latent_attend(const uzip_latent_cache *cache, uzip_dtype dtype, const void *d_q, int64_t q_row,
@@ -211,7 +211,7 @@ uzip_status uzip_latent_attend(const uzip_latent_cache *cache, uzip_dtype dtype,
   call.rows = latent_rows(n_rows, n_heads, max_new);
   a.part_acc = (float *)d_ws;
   a.part_ml = a.part_acc + (size_t)2 * kLatentUnits * call.rows * cache->latent;
-  a.cuts = (LatentCut *)(a.part_ml + (size_t)2 * kLatentUnits * call.rows * 2);
+  a.cuts = (LatentCut *)(a.part_ml + (size_t)2 * kLatentUnits * call.rows * 4);
   call.type = dtype;
   call.code = cache->dtype;
   call.stream = stream;

@@ -1,0 +1,106 @@
+"""GPU: the absorbed form where weights differ much: one token with most of the weight before thousands of small ones, weights all
+alike, against oracle/latent.py in 64 bits.
+
+Tolerance of an output, beside its own rounding (half an ulp) and the scores', exponentials' and sums' as in test_gpu_latent.py: a
+weight is off by 2^-9 (bf16, two terms of four bits) or 2^-14 (fp16, three) of itself, or by 2^-21 or 2^-25 of the largest
+weight of its 64 tokens (`tiles`), which is in [2^7, 2^8) where the last term's half step is 2^-14 or 2^-18; of eight products side by
+side what lies 2^-13 below the largest is dropped: 2^-10 of the sum of magnitudes of these eight.  Nothing in it grows with the number of tokens but the
+sums' own 2^-24 of each addition.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import latent as ref
+
+from test_gpu_latent import dev, ints, np_of
+from test_gpu_rotary import LEAST, TYPES, U_OUT
+
+pytestmark = pytest.mark.gpu
+
+U_W = {"bf16": 2.0 ** -9, "fp16": 2.0 ** -14}
+TILE = {"bf16": 2.0 ** -21, "fp16": 2.0 ** -25}
+
+
+@pytest.fixture(scope="module")
+def uz():
+    import paper_2604_17172_amd as m
+    return m
+
+
+def check_weights(got, want, kind, products, tokens, dropped):
+    """products: of a score, those that are not zero; dropped: of each output, the sum of magnitudes of groups of eight whose
+    products differ by more than 2^6, in p |c|."""
+    out, lse = got
+    out, lse = np_of(out), lse.cpu().numpy().astype(np.float64)
+    score = (products * 2.0 ** -24 + 2.0 ** -22) * want["size"] + 2.0 ** -21 + 2.0 ** -23 * want["shift"]
+    eps = 2 * (score + tokens * 2.0 ** -24)
+    assert eps.max() < 2.0 ** -6                                          # else nothing is tested
+    tol = U_OUT[kind] * np.abs(want["out"]) + (U_W[kind] + 2.0 ** -14 + eps)[..., None] * want["spread"] + TILE[kind] * want["tiles"]
+    tol = tol + 2.0 ** -10 * dropped + LEAST[kind]
+    off = np.abs(out - want["out"])
+    assert (off <= tol).all(), (np.argwhere(~(off <= tol))[:4].tolist(), np.nanmax(off / tol))
+    assert (np.abs(lse - want["lse"]) <= eps + 2.0 ** -22 * np.abs(want["lse"])).all()
+
+
+def attend(uz, codes, exps, rot, q, tokens, requests, scale, fmt="e4m3fn"):
+    """`requests` requests of the same pages and queries [heads, width], one new token each."""
+    page = codes.shape[1]
+    cache = uz.LatentCache(dev(codes), dev(exps), rot, fmt)
+    table = np.tile(np.arange(codes.shape[0], dtype=np.int32), (requests, 1))
+    rows = q[None].expand(requests, -1, -1).contiguous()
+    got = uz.latent_attend(rows, cache, ints(table), ints([tokens] * requests), ints(np.arange(requests + 1)), 1, scale)
+    torch.cuda.synchronize()
+    latent = codes.shape[2] - rot
+    want = ref.attend(np_of(rows[:1]), codes, exps, latent, fmt, table[:1], [tokens], [0, 1], page, scale)
+    return got, want
+
+
+def first_token_case(kind, latent, heads, tokens, share, g):
+    """Codes and exponents, and queries whose rotary part gives token 0 that share of the weight; its magnitude is in four channels, the other
+    tokens' latents point one way."""
+    rot, page, scale = 64, 64, 0.0625
+    pages = -(-tokens // page)
+    codes = g.integers(0x30, 0x41, (pages, page, latent + rot)).astype(np.uint8)  # 0.5 to 2.25
+    codes[..., :latent] |= (g.integers(0, 2, latent) << 7).astype(np.uint8)
+    codes[..., latent:] |= (g.integers(0, 2, (pages, page, rot)) << 7).astype(np.uint8)
+    codes[..., latent] = 0
+    exps = g.integers([117, 121], [120, 124], (pages, page, 2)).astype(np.uint8)
+    codes[0, 0] = 0
+    codes[0, 0, [3, 70, 130, 255]] = [0x70, 0xF1, 0x72, 0x73]
+    codes[0, 0, latent], exps[0, 0] = 0x38, [122, 127]                    # a rotary key of 1 in its first channel
+    q = np.zeros((heads, latent + rot))
+    q[:, latent + 1:] = g.standard_normal((heads, rot - 1)) * 8          # scores that differ by about 0.2
+    q[:, latent] = np.log(share * tokens / (1 - share)) / scale
+    return codes, exps, torch.from_numpy(q.astype(np.float32)).to(TYPES[kind]).cuda(), scale
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("tokens,share", [(8190, 0.7), (8190, 0.9), (16383, 0.5), (16383, 0.7), (60000, 0.5), (60000, 0.9)])
+@pytest.mark.parametrize("latent,heads,requests", [(512, 16, 256), (256, 64, 256), (512, 40, 3)])
+def test_small_weights_beside_a_large_one(uz, kind, tokens, share, latent, heads, requests):
+    """256 requests: a workgroup takes all of a request's tokens; 3: each is cut into pieces."""
+    print("[tail]", kind, tokens, share, latent, heads, requests, flush=True)
+    codes, exps, q, scale = first_token_case(kind, latent, heads, tokens, share, np.random.default_rng(61))
+    got, want = attend(uz, codes, exps, 64, q, tokens, requests, scale)
+    weight = np.exp(scale * np_of(q) @ np.eye(1, q.shape[1], latent)[0] - want["lse"][0])
+    assert (abs(weight - share) < 0.15).all()
+    sink = np.abs(ref.code_values("e4m3fn")[codes[0, 0, :latent]]) * 2.0 ** (122 - 127)
+    check_weights(got, want, kind, 63, tokens, weight[:, None] * sink)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
+@pytest.mark.parametrize("latent", [256, 512])
+def test_weights_that_are_alike_keep_their_bits(uz, kind, fmt, latent):
+    """All of a row's weights the same, 32 fractions of an octave over the heads: what a weight loses they lose alike."""
+    g, rot, heads, tokens, scale = np.random.default_rng(62), 64, 32, 640, 2.0 ** -7
+    one, least, most = {"e4m3fn": (0x38, 0x30, 0x41), "e5m2": (0x3C, 0x38, 0x41)}[fmt]
+    codes = g.integers(least, most, (10, 64, latent + rot)).astype(np.uint8)
+    codes[..., latent:] = 0
+    codes[..., latent] = one
+    exps = np.full((10, 64, 2), 127, np.uint8)
+    q = torch.zeros(heads, latent + rot, dtype=TYPES[kind], device="cuda")
+    q[:, latent] = torch.arange(heads) / 32 * np.log(2) / scale
+    got, want = attend(uz, codes, exps, rot, q, tokens, 1, scale, fmt)
+    check_weights(got, want, kind, 1, tokens, 0.0)
