@@ -274,7 +274,8 @@ struct LatentTile {
   float mul[kTile];                      // fp16: on the scores
   float e[kTile], inv[kTile];            // e_t, 2^-e_t
   uint64_t valid;                        // which tokens there are
-  uint8_t fill[248];                     // the next tile begins at a multiple of 256 bytes
+  uint32_t far;                          // whether some e_t are far from others
+  uint8_t fill[244];                     // the next tile begins at a multiple of 256 bytes
 };
 __device__ __forceinline__ uint32_t swizzle(uint32_t t) { return ((t & 3) << 1) | ((t >> 2) & 1) | (t & 8); }
 
@@ -550,6 +551,7 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
           }
           const int32_t t0 = (int32_t)((tile0 + i) * kTile);
           const uint64_t valid = lds.tile[i % L::kBufs].valid;
+          const bool far = uniform(lds.tile[i % L::kBufs].far) != 0;
           if (~valid || t0 + kTile - 1 > at_min) {
             const uint32_t there = (uint32_t)(valid >> (32 * half + 4 * h));
             const int32_t upto = at - t0 - 32 * (int)half - 4 * (int)h;
@@ -567,9 +569,10 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
           __syncthreads();
 
           // the reference of this tile's weights and of the sums, the factor on the sums so far, the weights
-          f32x4 inv[4];
+          f32x4 scales[4];  // 2^-e_t; e_t where some are far from others
+          const uint32_t at_scales = of_four + (far ? (uint32_t)offsetof(Tile, e) : (uint32_t)offsetof(Tile, inv));
 #pragma unroll
-          for (int g = 0; g < 4; ++g) inv[g] = *(LdsFloats)(uintptr_t)(of_four + offsetof(Tile, inv) + 32 * g);
+          for (int g = 0; g < 4; ++g) scales[g] = *(LdsFloats)(uintptr_t)(at_scales + 32 * g);
           most = fmaxf(lds.most[rg][0][col], lds.most[rg][1][col]);
           const float ref = __builtin_floorf(most) - L::kTop;
           const float next = ref > m + L::kLag ? ref : m;
@@ -577,16 +580,25 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
             lds.factor[i & 1][rg][col] = f32x2{next == m ? 1.0f : times_pow2(1.0f, m - next), __int_as_float(127 - kDown + (int)fmaxf(ref - next, kDown - 127.0f))};
           m = next;
           const float from = ref == -INFINITY ? 0.0f : ref;
-          float sum = 0;
+          float sum = 0;  // of the divisor's terms
+          if (far) {  // which are numbers where the weights may be none
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float x = s[e] - from;
+              sum += __builtin_amdgcn_exp2f(x - scales[e / 4][e % 4]);
+              s[e] = __builtin_amdgcn_exp2f(x);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              s[e] = __builtin_amdgcn_exp2f(s[e] - from);
+              sum = __builtin_fmaf(s[e], scales[e / 4][e % 4], sum);
+            }
+          }
           i32x4 w[TERMS];
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            float y[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              y[k] = __builtin_amdgcn_exp2f(s[4 * g + k] - from);
-              sum = __builtin_fmaf(y[k], inv[g][k], sum);
-            }
+            float y[4] = {s[4 * g], s[4 * g + 1], s[4 * g + 2], s[4 * g + 3]};
 #pragma unroll
             for (int term = 0; term < TERMS; ++term) {
               int code = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
@@ -692,7 +704,13 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
           }
           tile->e[lane] = (float)((int)ec - 127);
           tile->inv[lane] = pow2(254 - (int)ec);
-          if (lane == 0) tile->valid = n.valid;
+          // weights of up to 2^-134 of the largest are numbers: enough for the divisor where no two e_t are more than 100 apart
+          const int first = __builtin_amdgcn_readlane((int)ec, n.valid ? __ffsll((unsigned long long)n.valid) - 1 : 0);
+          const bool far = __any(ok && abs((int)ec - first) > 50);
+          if (lane == 0) {
+            tile->valid = n.valid;
+            tile->far = far;
+          }
         };
 
         Next then{};  // of tile i + 1

@@ -104,3 +104,34 @@ def test_weights_that_are_alike_keep_their_bits(uz, kind, fmt, latent):
     q[:, latent] = torch.arange(heads) / 32 * np.log(2) / scale
     got, want = attend(uz, codes, exps, rot, q, tokens, 1, scale, fmt)
     check_weights(got, want, kind, 1, tokens, 0.0)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
+@pytest.mark.parametrize("latent", [256, 512])
+@pytest.mark.parametrize("least,most,tokens", [(78, 163, 200), (27, 246, 64), (27, 246, 1000), (27, 80, 700), (110, 246, 130)])
+def test_scales_that_are_far_apart(uz, kind, fmt, latent, least, most, tokens):
+    """Latents of all sizes side by side, their scores alike: every token counts in the divisor, those of the largest scales make the
+    output."""
+    top = {"bf16": 246 if fmt == "e4m3fn" else 239, "fp16": 132 if fmt == "e4m3fn" else 125}[kind]  # outputs are within the type
+    most = min(most, top)
+    g, rot, page, scale = np.random.default_rng(63), 64, 16, 0.05
+    pages = -(-tokens // page)
+    codes = (g.integers(0, 256, (pages, page, latent + rot)) & 0xBB).astype(np.uint8)
+    exps = g.integers(least, most + 1, (pages, page, 2)).astype(np.uint8)
+    exps[..., 1] = {"e4m3fn": 125, "e5m2": 118}[fmt]
+    q = torch.zeros(24, latent + rot, dtype=TYPES[kind], device="cuda")
+    q[:, latent:] = torch.from_numpy(g.standard_normal((24, rot)).astype(np.float32))
+    for requests in (1, 300):
+        got, want = attend(uz, codes, exps, rot, q, tokens, requests, scale, fmt)
+        check_weights(got, want, kind, rot, tokens, want["spread"])
+
+
+@pytest.mark.parametrize("heads", [1, 40])
+def test_latents_of_zero(uz, heads):
+    """The least scale, in millions of tokens: the divisor is their number, of whose logarithm 22 rounding to 24 bits takes 2^-20 each time."""
+    page, latent, rot, pages = 256, 512, 64, 1 << 14
+    codes, exps = torch.zeros(1, page, latent + rot, dtype=torch.uint8, device="cuda"), torch.full((1, page, 2), 27, dtype=torch.uint8, device="cuda")
+    q = torch.randn(1, heads, latent + rot, device="cuda").to(torch.bfloat16)
+    out, lse = uz.latent_attend(q, uz.LatentCache(codes, exps, rot), ints(np.zeros((1, pages))), ints([pages * page]), ints([0, 1]), 1, 0.05)
+    assert (out == 0).all() and (lse.double() - np.log(pages * page)).abs().max() < 2.0 ** -18
