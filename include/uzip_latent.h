@@ -60,7 +60,8 @@ size_t uzip_latent_attend_workspace(uint32_t latent, uint32_t n_rows, uint32_t n
  * and sees the places 0 <= t <= p, as in uzip_kv_attend; out is [n_rows][n_heads][latent].
  *   out = sum_t e^(s_t) c_t / sum_t e^(s_t)    lse = log sum_t e^(s_t)
  * A row that sees nothing gives zeros and -infinity.  A token whose latent holds a NaN or an
- * infinity makes the rows that see it NaN, and no others.
+ * infinity makes the rows that see it NaN, and no others.  A rotary key that holds one counts by its
+ * score: minus infinity as no token, another one that is not finite makes its row NaN.
  * dtype is UZIP_BF16 or UZIP_FP16.  Scores and sums are held in 32 bits.  A weight enters the second
  * product with at least 8 bits for bf16, 12 for fp16, or off by at most 2^-21 (2^-25) of the
  * largest weight of its 64 tokens (those whose places are equal but for the last six

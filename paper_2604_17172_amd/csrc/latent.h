@@ -484,15 +484,16 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
         const int32_t at = here ? q.base + (int32_t)tok : -1;                                  // the row's place
         const int32_t at_min = q.base + (int32_t)a.by_heads.div(min(r0 + 32 * rg, list - 1));      // the first of the wave's rows
         const float scale_log2 = a.scale_log2;
+        const bool two = a.rot > 32;
         Eight query[2 * L::kSteps + 4];
         {
           const Value *src = (const Value *)a.q + (int64_t)(q.first + (int32_t)tok) * a.q_row + (int64_t)head * a.q_head;
-          const bool vec = a.q_vec, two = a.rot > 32;
+          const bool vec = a.q_vec;
 #pragma unroll
           for (int s = 0; s < 2 * L::kSteps + 4; ++s) {
             const uint32_t d = 32 * (s / 2) + 16 * h + 8 * (s % 2);
             Eight e;
-            if (!here || (s >= 2 * L::kSteps + 2 && !two)) {  // of 32 rotary channels the keys' second half holds the first once more
+            if (!here || (s >= 2 * L::kSteps + 2 && !two)) {
 #pragma unroll
               for (int j = 0; j < 8; ++j) e[j] = (Value)0.0f;
             } else if (vec) {
@@ -536,8 +537,11 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
             const u32x4 now = c[k % kAhead];
             if constexpr (k + kAhead < kReads) c[k % kAhead] = chunk(k + kAhead);
             const float scale = k < L::kSteps ? sc : sr;
-            s = mfma16(eight_codes<CODE, T>(now.x, now.y, scale), query[2 * k], s);
-            s = mfma16(eight_codes<CODE, T>(now.z, now.w, scale), query[2 * k + 1], s);
+            // (the last is of the rotary keys' second 32 channels: where there are none an infinity of the first would be times 0)
+            if (k <= L::kSteps || two) {
+              s = mfma16(eight_codes<CODE, T>(now.x, now.y, scale), query[2 * k], s);
+              s = mfma16(eight_codes<CODE, T>(now.z, now.w, scale), query[2 * k + 1], s);
+            }
             __builtin_amdgcn_sched_barrier(0);
           });
           // times log2(e), plus e_t; the largest

@@ -135,3 +135,23 @@ def test_latents_of_zero(uz, heads):
     q = torch.randn(1, heads, latent + rot, device="cuda").to(torch.bfloat16)
     out, lse = uz.latent_attend(q, uz.LatentCache(codes, exps, rot), ints(np.zeros((1, pages))), ints([pages * page]), ints([0, 1]), 1, 0.05)
     assert (out == 0).all() and (lse.double() - np.log(pages * page)).abs().max() < 2.0 ** -18
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("latent,rot", [(256, 32), (512, 32), (512, 64)])
+def test_an_infinite_rotary_key_counts_by_its_score(uz, kind, latent, rot):
+    """Minus infinity: as if the token were not there; plus infinity, or none since a query's channel is 0: no number."""
+    g, page, tokens, scale = np.random.default_rng(64), 16, 75, 0.05
+    codes = (g.integers(0, 256, (5, page, latent + rot)) & 0xBB).astype(np.uint8)
+    codes[..., latent:] &= 0xB7
+    exps = np.full((5, page, 2), 118, np.uint8)
+    codes[4, 10, latent + 9] = 0x7C                                       # the last token's
+    q = torch.from_numpy(g.standard_normal((40, latent + rot)).astype(np.float32)).to(TYPES[kind]).cuda()
+    q[20:, latent + 9] = q[20:, latent + 9].abs()
+    q[:20, latent + 9] = -q[:20, latent + 9].abs()
+    q[39, latent + 9] = 0
+    got, _ = attend(uz, codes, exps, rot, q, tokens, 2, scale, "e5m2")
+    codes[4, 10, latent + 9] = 0
+    _, want = attend(uz, codes, exps, rot, q[:20], tokens - 1, 1, scale, "e5m2")
+    check_weights((got[0][:, :20], got[1][:, :20]), want, kind, latent + rot, tokens, want["spread"])
+    assert torch.isnan(got[0][:, 20:]).all() and torch.isnan(got[1][:, 20:]).all()
