@@ -270,8 +270,7 @@ template <int DC>
 struct LatentTile {
   uint8_t latent[kTile * DC];
   uint8_t rot[kTile * 64];
-  float scale_c[kTile], scale_r[kTile];  // on the codes of the first product
-  float mul[kTile];                      // fp16: on the scores
+  float scale_c[kTile], scale_r[kTile];  // bf16: on the codes of the first product; fp16: on the products
   float e[kTile], inv[kTile];            // e_t, 2^-e_t
   uint64_t valid;                        // which tokens there are
   uint32_t far;                          // whether some e_t are far from others
@@ -518,16 +517,16 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
           if (careful) __syncthreads();
           const uint32_t tile = tiles0 + i % L::kBufs * (uint32_t)sizeof(Tile);
           const uint32_t of_token = tile + 4 * (32 * half + col), of_four = tile + 4 * (32 * half + 4 * h);
-          const float sc = *(LdsFloat)(uintptr_t)(of_token + offsetof(Tile, scale_c)), sr = *(LdsFloat)(uintptr_t)(of_token + offsetof(Tile, scale_r));
+          [[maybe_unused]] const float sc = *(LdsFloat)(uintptr_t)(of_token + offsetof(Tile, scale_c)), sr = *(LdsFloat)(uintptr_t)(of_token + offsetof(Tile, scale_r));
           const uint32_t k_at = tile + k_off, r_at = tile + r_off;
           // The order is written down, between barriers to the compiler's scheduler: reads some steps ahead.
           constexpr int kReads = L::kSteps + 2;
           auto chunk = [&](int k) {
             return k < L::kSteps ? *(LdsFour)(uintptr_t)((k_at ^ ((k & 7) << 5)) + (k >> 3) * 256) : *(LdsFour)(uintptr_t)(r_at ^ ((k - L::kSteps) << 5));
           };
-          f32x16 s;
+          f32x16 s, of_rot;  // fp16: the latents' and the rotary keys' products apart
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[e] = 0;
+          for (int e = 0; e < 16; ++e) s[e] = of_rot[e] = 0;
           u32x4 c[kAhead];
 #pragma unroll
           for (int k = 0; k < kAhead; ++k) c[k] = chunk(k);
@@ -536,11 +535,12 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
             constexpr int k = decltype(number)::value;
             const u32x4 now = c[k % kAhead];
             if constexpr (k + kAhead < kReads) c[k % kAhead] = chunk(k + kAhead);
-            const float scale = k < L::kSteps ? sc : sr;
+            const float scale = T == UZIP_FP16 ? 1.0f : k < L::kSteps ? sc : sr;
+            f32x16 &to = T == UZIP_FP16 && k >= L::kSteps ? of_rot : s;
             // (the last is of the rotary keys' second 32 channels: where there are none an infinity of the first would be times 0)
             if (k <= L::kSteps || two) {
-              s = mfma16(eight_codes<CODE, T>(now.x, now.y, scale), query[2 * k], s);
-              s = mfma16(eight_codes<CODE, T>(now.z, now.w, scale), query[2 * k + 1], s);
+              to = mfma16(eight_codes<CODE, T>(now.x, now.y, scale), query[2 * k], to);
+              to = mfma16(eight_codes<CODE, T>(now.z, now.w, scale), query[2 * k + 1], to);
             }
             __builtin_amdgcn_sched_barrier(0);
           });
@@ -548,10 +548,15 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const f32x4 e = *(LdsFloats)(uintptr_t)(of_four + offsetof(Tile, e) + 32 * g);
-            f32x4 mul;
-            if constexpr (T == UZIP_FP16) mul = *(LdsFloats)(uintptr_t)(of_four + offsetof(Tile, mul) + 32 * g);
+            if constexpr (T == UZIP_FP16) {
+              const f32x4 by_c = *(LdsFloats)(uintptr_t)(of_four + offsetof(Tile, scale_c) + 32 * g);
+              const f32x4 by_r = *(LdsFloats)(uintptr_t)(of_four + offsetof(Tile, scale_r) + 32 * g);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[4 * g + k] = __builtin_fmaf(s[4 * g + k], T == UZIP_FP16 ? mul[k] : scale_log2, e[k]);
+              for (int k = 0; k < 4; ++k) s[4 * g + k] = __builtin_fmaf(s[4 * g + k], by_c[k], __builtin_fmaf(of_rot[4 * g + k], by_r[k], e[k]));
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) s[4 * g + k] = __builtin_fmaf(s[4 * g + k], scale_log2, e[k]);
+            }
           }
           const int32_t t0 = (int32_t)((tile0 + i) * kTile);
           const uint64_t valid = lds.tile[i % L::kBufs].valid;
@@ -697,15 +702,9 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
           Tile *tile = &lds.tile[i % L::kBufs];
           const bool ok = n.valid >> lane & 1;
           const uint32_t ec = ok ? max(n.exps & 0xFF, 1u) : 127, er = ok ? max(n.exps >> 8 & 0xFF, 1u) : 127;
-          if constexpr (T == UZIP_FP16) {  // fp16 holds codes times powers of two up to 1
-            const uint32_t most = max(ec, er);
-            tile->scale_c[lane] = pow2(max(127 + (int)ec - (int)most, 1));
-            tile->scale_r[lane] = pow2(max(127 + (int)er - (int)most, 1));
-            tile->mul[lane] = a.scale_log2 * pow2(most);
-          } else {
-            tile->scale_c[lane] = pow2(ec);
-            tile->scale_r[lane] = pow2(er);
-          }
+          // fp16 holds the codes themselves, but not codes of latents and rotary keys whose scales differ by 2^15 or more
+          tile->scale_c[lane] = T == UZIP_FP16 ? a.scale_log2 * pow2(ec) : pow2(ec);
+          tile->scale_r[lane] = T == UZIP_FP16 ? a.scale_log2 * pow2(er) : pow2(er);
           tile->e[lane] = (float)((int)ec - 127);
           tile->inv[lane] = pow2(254 - (int)ec);
           // weights of up to 2^-134 of the largest are numbers: enough for the divisor where no two e_t are more than 100 apart

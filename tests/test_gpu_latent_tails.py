@@ -155,3 +155,19 @@ def test_an_infinite_rotary_key_counts_by_its_score(uz, kind, latent, rot):
     _, want = attend(uz, codes, exps, rot, q[:20], tokens - 1, 1, scale, "e5m2")
     check_weights((got[0][:, :20], got[1][:, :20]), want, kind, latent + rot, tokens, want["spread"])
     assert torch.isnan(got[0][:, 20:]).all() and torch.isnan(got[1][:, 20:]).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("fmt", ["e4m3fn", "e5m2"])
+@pytest.mark.parametrize("latent,heads", [(256, 24), (512, 64)])
+@pytest.mark.parametrize("of_latent,of_rot", [(-18, 2), (-19, 7), (2, -18), (9, -17)])
+def test_scores_of_latents_and_rotary_keys_of_unlike_sizes(uz, kind, fmt, latent, heads, of_latent, of_rot):
+    """Latents of 2^20 to 2^26 times the rotary keys' size or the other way round, queries so that both parts of a score are alike: a
+    score is a sum of exact products in 32 bits."""
+    g, rot, page, tokens, scale = np.random.default_rng(65), 64, 16, 130, 4.0
+    codes = g.integers(0, 256, (9, page, latent + rot)) & 0xBF        # magnitudes below 2
+    exps = np.full((9, page, 2), [127 + of_latent, 127 + of_rot], np.uint8)
+    part = np.repeat([2.0 ** -(6 + of_latent + (latent == 512) / 2), 2.0 ** -(5 + of_rot)], [latent, rot])  # within fp16
+    q = torch.from_numpy((g.standard_normal((heads, latent + rot)) * part).astype(np.float32)).to(TYPES[kind]).cuda()
+    got, want = attend(uz, codes.astype(np.uint8), exps.astype(np.uint8), rot, q, tokens, 2, scale, fmt)
+    check_weights(got, want, kind, latent + rot, tokens, want["spread"])
