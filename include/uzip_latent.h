@@ -82,8 +82,10 @@ uzip_status uzip_latent_attend(const uzip_latent_cache *cache, uzip_dtype dtype,
  * d_q_start[i] .. d_q_start[i + 1], its keys d_k_start[i] .. d_k_start[i + 1]; row j of n_i
  * stands at place (its keys) - n_i + j among them and sees the places up to its own.
  * nope and value are 64 or 128, rot 32 or 64; dtype is UZIP_BF16 or UZIP_FP16.  Scores and sums are
- * held in 32 bits; weights enter the second product in dtype.  A row that sees nothing gives zeros
- * and -infinity.  A value that is infinite or NaN reaches the rows that see it, and no others.
+ * held in 32 bits; weights enter the second product in dtype, fp16 with its 11 bits down to
+ * 2^-21 of the row's largest and off by at most 2^-32 of that below.  A row that sees nothing
+ * gives zeros and -infinity.  A value that is infinite or NaN reaches the rows that see it, and
+ * no others.
  *   max_new:  the most new tokens of a request: it chooses kernels, a wrong value costs
  *             time and the last bits may differ.
  *   d_lse:    [n_rows][n_heads] (may be NULL).

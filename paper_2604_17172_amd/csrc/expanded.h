@@ -229,7 +229,10 @@ __global__ __launch_bounds__(64 * RG * SPLIT, RG * SPLIT / 4) void expanded_kern
   f32x16 acc[R][kBlocks], s[2][R];  // scores of this round's tile and of the next
   u32x4 w[R][2];
   float m[R], l[R], most[R], ref[R];
-  float lift = 0;  // weights are 2^-lift times as large
+  // Weights are 2^-lift times as large: in fp16 as large as they may be, since what is below 2^-25 becomes nothing.  (Past 2^24 a
+  // reference 7 less could come out 8 less or more, and a weight past 2^16.)
+  float lift = T == UZIP_FP16 ? kLag - 15 : 0;
+  auto lifted = [&](float m) { return T == UZIP_FP16 && fabsf(m) >= 0x1p24f ? m : m + lift; };
   // `count` steps, each with a read from LDS: two are on their way while the two before them are used, and
   // beside(i) is what the vector units do meanwhile.  The order is the one written here: the wave has its SIMD for
   // itself, and only what stands beside a matrix instruction runs beside it.
@@ -285,11 +288,11 @@ __global__ __launch_bounds__(64 * RG * SPLIT, RG * SPLIT / 4) void expanded_kern
   auto settle = [&] {
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      if (__any(most[r] > m[r] + kLag)) {
+      if (__any(most[r] - m[r] > kLag)) {
         const float both = max_of_halves(most[r]);
-        const float next = both > m[r] + kLag ? both : m[r], f = next == m[r] ? 1.0f : __builtin_amdgcn_exp2f(m[r] - next);
+        const float next = both - m[r] > kLag ? both : m[r], f = next == m[r] ? 1.0f : __builtin_amdgcn_exp2f(m[r] - next);
         m[r] = next;
-        ref[r] = next == -INFINITY ? 0.0f : next + lift;
+        ref[r] = next == -INFINITY ? 0.0f : lifted(next);
         l[r] *= f;
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n)
@@ -472,7 +475,7 @@ __global__ __launch_bounds__(64 * RG * SPLIT, RG * SPLIT / 4) void expanded_kern
   for (int r = 0; r < R; ++r) {
     const uint32_t j = 32 * (R * rg + r) + col;
     l[r] = sum_of_halves(l[r]);
-    m[r] += lift;
+    m[r] = lifted(m[r]);
     if (h == 0) {
       join.m[group][j] = m[r];
       join.l[group][j] = l[r];

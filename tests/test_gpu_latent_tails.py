@@ -171,3 +171,32 @@ def test_scores_of_latents_and_rotary_keys_of_unlike_sizes(uz, kind, fmt, latent
     q = torch.from_numpy((g.standard_normal((heads, latent + rot)) * part).astype(np.float32)).to(TYPES[kind]).cuda()
     got, want = attend(uz, codes.astype(np.uint8), exps.astype(np.uint8), rot, q, tokens, 2, scale, fmt)
     check_weights(got, want, kind, latent + rot, tokens, want["spread"])
+
+
+@pytest.mark.parametrize("nope,rot,value,heads,tokens", [(128, 64, 128, 3, 60000), (64, 32, 64, 200, 3000), (64, 32, 64, 70, 9000), (64, 64, 64, 2, 200000)])
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+def test_expanded_small_weights_beside_a_large_one(uz, kind, nope, rot, value, heads, tokens):
+    """Keys after the first that weigh 2^-25.5 of it: a weight is a number of the type, in fp16 with 11 bits down to 2^-21 of the largest, and
+    off by at most 2^-32 of it below."""
+    g, scale, rows = np.random.default_rng(66), 2.0 ** -5, 65
+    k = torch.zeros(tokens, heads, nope, dtype=TYPES[kind], device="cuda")
+    k[0, :, 0] = 16
+    v = torch.rand(tokens, heads, value, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).add_(0.5).to(TYPES[kind])
+    v[0] = 0                                                              # what there is comes from the others
+    q = torch.zeros(rows, heads, nope + rot, dtype=TYPES[kind], device="cuda")
+    q[..., 0] = torch.from_numpy(25.5 * np.log(2) / 16 / scale + g.standard_normal((rows, heads)) * 0.1).cuda()
+    r = torch.zeros(tokens, rot, dtype=TYPES[kind], device="cuda")
+    out, lse = uz.latent_attend_expanded(q, k, r, v, ints([0, rows]), ints([0, tokens]), rows, scale=scale)
+    torch.cuda.synchronize()
+    first = np_of(q[..., 0]) * 16 * scale                                 # the others' scores are 0
+    seen = (tokens - rows + 1 + np.arange(rows))[:, None]
+    total = np.exp(first) + seen - 1
+    sums = v.double().cumsum(0)[tokens - rows:].cpu().numpy()
+    want = sums / total[..., None]
+    # beside the rounding of an output: a weight's, the exponential's and the score's, the sums'
+    eps = 2.0 ** -21 + 2.0 ** -22 * first.max() + 2 * tokens * 2.0 ** -24
+    tol = U_OUT[kind] * want + ({"bf16": 2.0 ** -8, "fp16": 2.0 ** -11}[kind] + 2 * eps) * want + LEAST[kind]
+    if kind == "fp16":
+        tol = tol + 2.0 ** -32 * sums
+    assert (np.abs(np_of(out) - want) <= tol).all(), np.nanmax(np.abs(np_of(out) - want) / tol)
+    assert (np.abs(lse.cpu().numpy() - np.log(total)) <= 2 * eps + 2.0 ** -22 * np.log(total)).all()
