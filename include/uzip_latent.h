@@ -86,6 +86,8 @@ uzip_status uzip_latent_attend(const uzip_latent_cache *cache, uzip_dtype dtype,
  * 2^-21 of the row's largest and off by at most 2^-32 of that below.  A row that sees nothing
  * gives zeros and -infinity.  A value that is infinite or NaN reaches the rows that see it, and
  * no others.
+ * Scores are not to pass 2^24, where 32 bits hold whole numbers: weights, powers of two of their
+ * differences, may then pass what they are held in.
  *   max_new:  the most new tokens of a request: it chooses kernels, a wrong value costs
  *             time and the last bits may differ.
  *   d_lse:    [n_rows][n_heads] (may be NULL).

@@ -200,3 +200,21 @@ def test_expanded_small_weights_beside_a_large_one(uz, kind, nope, rot, value, h
         tol = tol + 2.0 ** -32 * sums
     assert (np.abs(np_of(out) - want) <= tol).all(), np.nanmax(np.abs(np_of(out) - want) / tol)
     assert (np.abs(lse.cpu().numpy() - np.log(total)) <= 2 * eps + 2.0 ** -22 * np.log(total)).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("power", [12, 16, 18, 20, 22, 23, 24, 26, 30])
+def test_scores_past_what_32_bits_tell_apart(uz, kind, power):
+    """Scores of up to 2^34, where a reference some powers of two from them is rounded, and up to 2^24 for the expanded form: outputs are
+    means of what a row sees."""
+    g, scale, tokens = np.random.default_rng(67), 2.0 ** power, 300
+    x = lambda *s: torch.from_numpy(g.standard_normal(s).astype(np.float32)).to(TYPES[kind]).cuda()  # noqa: E731
+    codes = (g.integers(0, 256, (20, 16, 288)) & 0xBB).astype(np.uint8)
+    exps = g.integers(118, 124, (20, 16, 2)).astype(np.uint8)
+    got, want = attend(uz, codes, exps, 32, x(40, 288), 310, 2, scale)
+    values = np.abs(ref.code_values("e4m3fn")[codes[..., :256]] * 2.0 ** (exps[..., :1].astype(np.float64) - 127)).reshape(-1, 256)[:310]
+    assert (np.abs(np_of(got[0])) <= values.max(axis=0) * (1 + 2.0 ** -7)).all() and torch.isfinite(got[1]).all()
+    k, v, r, q = x(tokens, 100, 64), x(tokens, 100, 64), x(tokens, 32), x(tokens, 100, 96)
+    out, lse = uz.latent_attend_expanded(q, k, r, v, ints([0, tokens]), ints([0, tokens]), tokens, scale=min(scale, 2.0 ** 18))
+    most = v.float().abs().cummax(0).values
+    assert (out.float().abs() <= most * (1 + 2.0 ** -7)).all() and torch.isfinite(lse).all()
