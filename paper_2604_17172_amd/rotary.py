@@ -66,7 +66,7 @@ def rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", f
 
         def number(turns):                                      # of the pair that turns so often over the trained length
             return rot * math.log(trained / (turns * 2 * math.pi)) / (2 * math.log(base))
-        low, high = max(math.floor(number(fast)), 0), min(math.ceil(number(slow)), rot // 2 - 1)
+        low, high = max(math.floor(number(fast)), 0), min(math.ceil(number(slow)), rot - 1)   # may lie past the last pair
         divided = ((i - low) / max(high - low, 1e-3)).clamp(0, 1)
         freq = freq * (1 - divided) + freq / factor * divided
         magnitude = 0.1 * math.log(factor) + 1

@@ -144,6 +144,24 @@ def test_frequencies(uz):
             uz.rotary_frequencies(*args, device="cpu")
 
 
+@pytest.mark.parametrize("rot,trained", [(64, 131072), (128, 131072), (64, 65536), (96, 1 << 20), (64, 4096), (32, 1 << 22)])
+def test_frequencies_of_long_trained_contexts(uz, rot, trained):
+    """The slowest pairs turn more than once over the trained length: none of them is divided by the whole factor."""
+    factor, base = 4.0, 10000.0
+    plain, _ = uz.rotary_frequencies(rot, base, device="cpu")
+    got, _ = uz.rotary_frequencies(rot, base, "parts", factor, trained, device="cpu")
+    turns = [trained * base ** (-2 * i / rot) / (2 * np.pi) for i in range(rot // 2)]
+
+    def number(t):                                                        # trained * base^(-2 n / rot) = 2 pi t
+        return rot / 2 * np.log(trained / (2 * np.pi * t)) / np.log(base)
+    low, high = max(np.floor(number(32)), 0), np.ceil(number(1))
+    for i in range(rot // 2):
+        part = min(max((i - low) / (high - low), 0), 1)
+        ratio = float(got[i] / plain[i])
+        assert abs(ratio - (1 - part + part / factor)) < 2.0 ** -22
+        assert ratio > 1 / factor + 1e-3 or turns[i] < 1
+
+
 # ------------------------------------------------------------------ the oracles
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_rotation_keeps_lengths_and_its_inverse_is_its_gradient(interleaved):
