@@ -354,6 +354,11 @@ struct Sum {
     unit = to;
   }
 };
+// The natural logarithm of x 2^unit, the same bits however the two are shared out: that depends on the wave's other rows.
+__device__ __forceinline__ float log_of(float x, float unit) {
+  const int e = __builtin_amdgcn_frexp_expf(x);
+  return (unit + (float)e + __builtin_amdgcn_logf(__builtin_ldexpf(x, -e))) * 0.69314718055994530942f;
+}
 // x, from which nothing is computed before this place: what only a seldom taken branch needs would else be
 // kept in registers through the loop around it.
 __device__ __forceinline__ uint32_t only_here(uint32_t x) {
@@ -846,7 +851,7 @@ __global__ __launch_bounds__(256 * RG, RG) void latent_kernel(LatentArgs args) {
                 }
               }
             if (half == 0 && h == 0 && a.lse)
-              a.lse[(size_t)(q.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (unit + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+              a.lse[(size_t)(q.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : log_of(l, unit);
           } else {
             const size_t slot = 2 * (size_t)blockIdx.x + (begin > place.before ? 0 : 1), row = slot * L::kRows + 32 * rg + col;
             f32x4 *part = (f32x4 *)a.part_acc + (((slot * RG + rg) * 2 + half) * L::kBlocks * 4) * 64 + 32 * h + col;  // as the lanes hold them
@@ -927,7 +932,7 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentArgs a) {
     for (int e = 0; e < 4; ++e) out[e] = y[e];
   }
   if (blockIdx.y % (2 * kBlocks) == 0 && g == 0 && h == 0 && a.lse)
-    a.lse[(size_t)(c.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : (sum.unit + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    a.lse[(size_t)(c.first + (int32_t)tok) * a.heads + head] = l == 0 ? -INFINITY : log_of(l, sum.unit);
 }
 
 }  // namespace uzip_kv

@@ -12,6 +12,7 @@ import pytest
 import torch
 
 from oracle import latent as ref
+from oracle.kv import encode
 
 from test_gpu_latent import dev, ints, np_of
 from test_gpu_rotary import LEAST, TYPES, U_OUT
@@ -218,3 +219,24 @@ def test_scores_past_what_32_bits_tell_apart(uz, kind, power):
     out, lse = uz.latent_attend_expanded(q, k, r, v, ints([0, tokens]), ints([0, tokens]), tokens, scale=min(scale, 2.0 ** 18))
     most = v.float().abs().cummax(0).values
     assert (out.float().abs() <= most * (1 + 2.0 ** -7)).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads", [3, 16, 40])
+def test_what_a_workspace_held_changes_no_bit(uz, kind, heads):
+    g, latent, rot, tokens = np.random.default_rng(68), 512, 64, 3000
+    codes = (g.integers(0, 256, (47, 64, latent + rot)) & 0xBB).astype(np.uint8)
+    exps = g.integers(110, 124, (47, 64, 2)).astype(np.uint8)
+    codes[..., latent], exps[..., 1] = encode(np.arange(47) / 8, "e4m3fn")[:, None], 127  # weights that grow from piece to piece
+    cache = uz.LatentCache(dev(codes), dev(exps), rot)
+    q = torch.from_numpy(g.standard_normal((2, heads, latent + rot)).astype(np.float32)).to(TYPES[kind]).cuda()
+    q[..., latent:] = 0
+    q[..., latent] = 500
+    table, lens, q_start = ints(np.tile(np.arange(47), (2, 1))), ints([tokens, 70]), ints([0, 1, 2])
+    ws = uz.latent_attend_workspace(q, cache, 2, 1)
+    first = None
+    for fill in (0, 0x01, 0x3F, 0x7F, 0x80, 0xC2, 0xFF):
+        ws.fill_(fill)
+        got = uz.latent_attend(q, cache, table, lens, q_start, 1, 0.004, ws=ws)
+        first = first or got
+        assert torch.equal(got[0], first[0]) and torch.equal(got[1], first[1]), fill
