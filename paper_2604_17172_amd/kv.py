@@ -181,6 +181,16 @@ def _rows(x: torch.Tensor, name: str, dim: int, device: int) -> int:
     return t
 
 
+_increment = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
+
+
+def _wrote(*given) -> None:
+    """A kernel wrote to tensors of the caller's: autograd refuses what it saved of them before."""
+    written = [x for x in given if x is not None]
+    if written:
+        _increment(written)
+
+
 def _current(cache: KVCache) -> int:
     device = _device()
     if cache.index != device:

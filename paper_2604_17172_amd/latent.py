@@ -14,7 +14,7 @@ import ctypes
 import torch
 
 from . import BF16, EINVAL, FP16, OK, _check, _dev_empty, _lib
-from .kv import _CODES, _TYPES, _device, _handle, _i64, _int, _ints, _need, _on, _rows, _sz, _u32, _vp, _f32
+from .kv import _CODES, _TYPES, _device, _handle, _i64, _int, _ints, _need, _on, _rows, _sz, _u32, _vp, _f32, _wrote
 from .rotary import _queries, _query_args, _serves, _turn, _turn_p
 
 _c = ctypes
@@ -107,11 +107,13 @@ def latent_store(cache: LatentCache, latent: torch.Tensor, key_rot: torch.Tensor
     turn = _turn(positions, freq, rows, device, interleaved, 0, magnitude, False)
     if turn.rot != cache.rot:
         raise ValueError("freq is for the cache's rotary keys")
+    given = q_out
     q, q_out = _queries(q, q_out, rows, cache.rot, device, t, stream)
     rc = uzip_latent_store(cache, t, latent.data_ptr(), latent.stride(0), key_rot.data_ptr(), key_rot.stride(0), rows, slots.data_ptr(),
                            _c.byref(turn), *_query_args(q, q_out), _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_latent_store")
+    _wrote(given)
     return q_out
 
 
@@ -148,6 +150,7 @@ def latent_attend(q: torch.Tensor, cache: LatentCache, table: torch.Tensor, lens
         raise ValueError("table, lens and q_start are of one batch")
     if not 0 <= max_new < 1 << 32:
         raise ValueError("max_new is not negative")
+    given = out, lse
     if out is None or lse is None or ws is None:
         with _on(stream):
             out = torch.empty(rows, heads, cache.latent, dtype=q.dtype, device=q.device) if out is None else out
@@ -164,6 +167,7 @@ def latent_attend(q: torch.Tensor, cache: LatentCache, table: torch.Tensor, lens
                             ws.data_ptr(), ws.numel() * ws.element_size(), _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_latent_attend")
+    _wrote(*given)
     return out, lse
 
 
@@ -191,6 +195,7 @@ def latent_attend_expanded(q: torch.Tensor, k: torch.Tensor, key_rot: torch.Tens
         raise ValueError("q_start and k_start are of one batch")
     if not 0 <= max_new < 1 << 32:
         raise ValueError("max_new is not negative")
+    given = out, lse
     if out is None or lse is None:
         with _on(stream):
             out = torch.empty(rows, heads, value, dtype=q.dtype, device=q.device) if out is None else out
@@ -205,4 +210,5 @@ def latent_attend_expanded(q: torch.Tensor, k: torch.Tensor, key_rot: torch.Tens
                                      out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(), _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_latent_attend_expanded")
+    _wrote(*given)
     return out, lse

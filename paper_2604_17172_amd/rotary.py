@@ -14,7 +14,7 @@ import math
 import torch
 
 from . import OK, _check, _lib
-from .kv import KVCache, _TYPES, _cache_p, _current, _device, _handle, _i64, _int, _ints, _on, _rows, _u32, _vp
+from .kv import KVCache, _TYPES, _cache_p, _current, _device, _handle, _i64, _int, _ints, _on, _rows, _u32, _vp, _wrote
 
 _c = ctypes
 
@@ -96,6 +96,7 @@ def kv_positions(lens: torch.Tensor, q_start: torch.Tensor, rows: int, out: torc
         raise ValueError("lens and q_start are of one batch")
     if not 0 <= rows < 1 << 31:
         raise ValueError("rows is not negative")
+    given = out
     if out is None:
         with _on(stream):
             out = torch.empty(rows, dtype=torch.int32, device=lens.device)
@@ -105,6 +106,7 @@ def kv_positions(lens: torch.Tensor, q_start: torch.Tensor, rows: int, out: torc
     rc = uzip_kv_positions(lens.data_ptr(), q_start.data_ptr(), lens.numel(), rows, out.data_ptr(), _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_kv_positions")
+    _wrote(given)
     return out
 
 
@@ -117,6 +119,7 @@ def _rotate(x, positions, freq, interleaved, first, magnitude, inverse, out, str
     turn = _turn(positions, freq, rows, device, interleaved, first, magnitude, inverse)
     if first + turn.rot > dim:
         raise ValueError("the rotary part lies within dim")
+    given = out
     if out is None:
         with _on(stream):
             out = torch.empty(rows, heads, dim, dtype=x.dtype, device=x.device)
@@ -126,6 +129,7 @@ def _rotate(x, positions, freq, interleaved, first, magnitude, inverse, out, str
                      out.stride(1), _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_rotate")
+    _wrote(given)
     return out
 
 
@@ -208,6 +212,7 @@ def kv_rotate_store(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions:
     turn = _turn(positions, freq, rows, device, interleaved, first, magnitude, False)
     if first + turn.rot > cache.dim:
         raise ValueError("the rotary part lies within dim")
+    given = q_out
     q, q_out = _queries(q, q_out, rows, cache.dim, device, t, stream)
     k_step, v_step = k.stride(), v.stride()
     rc = uzip_kv_rotate_store(cache, t, k.data_ptr(), k_step[0], k_step[1], v.data_ptr(), v_step[0], v_step[1], rows,
@@ -215,4 +220,5 @@ def kv_rotate_store(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions:
                               _handle(stream, device))
     if rc != OK:
         _check(rc, "uzip_kv_rotate_store")
+    _wrote(given)
     return q_out

@@ -1,0 +1,57 @@
+"""GPU: rotary positions and latent attention among autograd's tensors: outputs that the caller gave, tangents, gradients that no call
+gives."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_rotary import TYPES, dev, freq_of, ints, rows_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def uz():
+    import paper_2604_17172_amd as m
+    return m
+
+
+def test_what_autograd_saved_is_not_changed_unseen(uz):
+    x, freq = torch.randn(3, 2, 32, device="cuda", requires_grad=True), dev(freq_of(32))
+    lens, q_start, places = ints([10]), ints([0, 3]), ints([0, 0, 0])
+    uz.kv_positions(lens, q_start, 3, out=places)
+    y = uz.rotate(x, places, freq)
+    uz.kv_positions(ints([20]), q_start, 3, out=places)                   # the next step's
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    w = x * 2
+    z = (w * w).sum()
+    with torch.no_grad():
+        uz.rotate(w, places, freq, out=w)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        z.backward()
+
+
+def test_versions_of_given_outputs(uz):
+    g = np.random.default_rng(0)
+    h = lambda *s: rows_of(s, "bf16", g)  # noqa: E731
+    freq, places, slots = dev(freq_of(32)), ints([0, 1]), torch.tensor([0, 1], device="cuda")
+    cache, pages = uz.LatentCache.empty(1, 256, 32, 16), uz.KVCache.empty(1, 1, 64, 16)
+    cache.codes.zero_()
+    cache.exps.fill_(127)
+    table, lens, q_start = ints([[0]]), ints([2]), ints([0, 2])
+    out, lse, wide, q_out = h(2, 3, 256), torch.zeros(2, 3, device="cuda"), h(2, 3, 64), h(2, 3, 32)
+    calls = [
+        ((q_out,), lambda: uz.rotate(h(2, 3, 32), places, freq, out=q_out)),
+        ((places,), lambda: uz.kv_positions(lens, q_start, 2, out=places)),
+        ((wide,), lambda: uz.kv_rotate_store(pages, h(2, 1, 64), h(2, 1, 64), places, freq, slots, ints([[0, 2]]), ints([1, 1]), q=h(2, 3, 64), q_out=wide)),
+        ((q_out,), lambda: uz.latent_store(cache, h(2, 1, 256)[:, 0], h(2, 1, 32)[:, 0], places, freq, slots, q=h(2, 3, 32), q_out=q_out)),
+        ((out, lse), lambda: uz.latent_attend(h(2, 3, 288), cache, table, lens, q_start, 2, 0.1, out=out, lse=lse)),
+        ((wide, lse), lambda: uz.latent_attend_expanded(h(2, 3, 96), h(2, 3, 64), h(2, 1, 32)[:, 0], h(2, 3, 64), q_start, q_start, 2, out=wide, lse=lse)),
+    ]
+    for given, call in calls:
+        before = [x._version for x in given]
+        call()
+        assert all(x._version > v for x, v in zip(given, before))
+        with torch.inference_mode():
+            call()
+    torch.cuda.synchronize()
