@@ -12,6 +12,7 @@ import ctypes
 import math
 
 import torch
+import torch.autograd.forward_ad as _forward
 
 from . import OK, _check, _lib
 from .kv import KVCache, _TYPES, _cache_p, _current, _device, _handle, _i64, _int, _ints, _on, _rows, _u32, _vp, _wrote
@@ -133,10 +134,16 @@ def _rotate(x, positions, freq, interleaved, first, magnitude, inverse, out, str
     return out
 
 
+def _followed(x) -> bool:
+    """Whether autograd follows x, backwards or forwards."""
+    return (x.requires_grad and torch.is_grad_enabled()) or (_forward._current_level >= 0 and _forward.unpack_dual(x).tangent is not None)
+
+
 class _Rotate(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, positions, freq, interleaved, first, magnitude, inverse):
         ctx.save_for_backward(positions, freq)
+        ctx.save_for_forward(positions, freq)
         ctx.how = interleaved, first, magnitude, inverse
         return _rotate(x, positions, freq, interleaved, first, magnitude, inverse, None, None)
 
@@ -149,13 +156,20 @@ class _Rotate(torch.autograd.Function):
         # through apply, so that a gradient of the gradient is had the same way
         return _Rotate.apply(grad, positions, freq, interleaved, first, magnitude, not inverse), None, None, None, None, None, None
 
+    @staticmethod
+    def jvp(ctx, tangent, *_):
+        positions, freq = ctx.saved_tensors
+        if tangent.stride(2) != 1:
+            tangent = tangent.contiguous()
+        return _Rotate.apply(tangent, positions, freq, *ctx.how)          # linear in x
+
 
 def rotate(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, interleaved: bool = False, first: int = 0,
            magnitude: float = 1.0, inverse: bool = False, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """x [rows, heads, dim] with channels first .. first + 2 freq.numel() turned by positions[row] * freq: pairs
     (i, i + rot / 2), or (2 i, 2 i + 1) where ``interleaved``, times ``magnitude``; by the angles' negatives with
     ``inverse``.  ``out`` may be x.  Differentiable in x where neither out nor stream is given."""
-    if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
+    if _followed(x) or (out is not None and _followed(out)):
         if out is not None or stream is not None:
             raise ValueError("a rotation that is differentiated takes neither out nor stream")
         return _Rotate.apply(x, positions, freq, interleaved, first, magnitude, inverse)
@@ -163,10 +177,9 @@ def rotate(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, interle
 
 
 def _serves(*tensors) -> None:
-    if torch.is_grad_enabled():
-        for x in tensors:
-            if x is not None and x.requires_grad:
-                raise ValueError("no gradient goes through this call: detach its inputs, or call it under torch.no_grad()")
+    for x in tensors:
+        if x is not None and _followed(x):
+            raise ValueError("no gradient goes through this call: detach its inputs, or call it under torch.no_grad()")
 
 
 def _queries(q, q_out, rows: int, dim: int, device: int, kind: int, stream):

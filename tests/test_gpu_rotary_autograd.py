@@ -55,3 +55,38 @@ def test_versions_of_given_outputs(uz):
         with torch.inference_mode():
             call()
     torch.cuda.synchronize()
+
+
+def test_tangents(uz):
+    """Forward derivatives: the operator of the tangent, also of a gradient; calls that serve refuse dual tensors."""
+    import torch.autograd.forward_ad as fw
+    g = np.random.default_rng(1)
+    x, t, up = (rows_of((4, 3, 40), "fp32", g) for _ in range(3))
+    places, freq = ints([3, 70, 9, 1]), dev(freq_of(32))
+    how = dict(interleaved=True, first=4, magnitude=1.5)
+    with fw.dual_level():
+        for tangent in (t, t[:, :1].expand(-1, 3, -1), t.transpose(0, 2).contiguous().transpose(0, 2)):
+            y = uz.rotate(fw.make_dual(x, tangent), places, freq, **how)
+            assert torch.equal(fw.unpack_dual(y).tangent, uz.rotate(tangent.contiguous(), places, freq, **how))
+            assert torch.equal(fw.unpack_dual(y).primal, uz.rotate(x, places, freq, **how))
+        with torch.no_grad():
+            assert fw.unpack_dual(uz.rotate(fw.make_dual(x, t), places, freq, **how)).tangent is not None
+        w = x.clone().requires_grad_(True)
+        y = uz.rotate(fw.make_dual(w, t), places, freq, **how)
+        grad, = torch.autograd.grad(y, w, fw.make_dual(up, t))
+        assert torch.equal(fw.unpack_dual(grad).tangent, uz.rotate(t, places, freq, inverse=True, **how))
+        dual = fw.make_dual(x, t)
+        with pytest.raises(ValueError):
+            uz.rotate(dual, places, freq, out=torch.empty_like(x))
+        h = lambda *s: rows_of(s, "bf16", g)  # noqa: E731
+        d = lambda *s: fw.make_dual(h(*s), h(*s))  # noqa: E731
+        pages, cache, slots, q_start = uz.KVCache.empty(1, 1, 64, 16), uz.LatentCache.empty(1, 256, 32, 16), torch.tensor([0, 1], device="cuda"), ints([0, 2])
+        two = ints([0, 1])
+        for call in (
+                lambda: uz.kv_rotate_store(pages, d(2, 1, 64), h(2, 1, 64), two, freq, slots, ints([[0, 2]]), ints([1, 1])),
+                lambda: uz.kv_rotate_store(pages, h(2, 1, 64), h(2, 1, 64), two, freq, slots, ints([[0, 2]]), ints([1, 1]), q=d(2, 3, 64)),
+                lambda: uz.latent_store(cache, d(2, 1, 256)[:, 0], h(2, 1, 32)[:, 0], two, freq, slots),
+                lambda: uz.latent_attend(d(2, 3, 288), cache, ints([[0]]), ints([2]), q_start, 2, 0.1),
+                lambda: uz.latent_attend_expanded(h(2, 3, 96), h(2, 3, 64), h(2, 1, 32)[:, 0], d(2, 3, 64), q_start, q_start, 2)):
+            with pytest.raises(ValueError, match="no gradient"):
+                call()

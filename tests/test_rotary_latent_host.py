@@ -194,3 +194,20 @@ def test_both_forms_of_latent_attention_agree():
     k, v = np.einsum("tl,hnl->thn", x[:, :latent], up_k), np.einsum("tl,hvl->thv", x[:, :latent], up_v)
     e = ref_latent.expanded(q, k, x[:, latent:], v, q_start, [0, 10, 17], 0.01)
     assert np.allclose(a["lse"], e["lse"], rtol=1e-12) and np.allclose(np.einsum("rhl,hvl->rhv", a["out"], up_v), e["out"], rtol=1e-9, atol=1e-12)
+
+
+# ------------------------------------------------------------------ autograd
+def test_calls_that_serve_refuse_what_autograd_follows(uz):
+    import torch.autograd.forward_ad as fw
+    from paper_2604_17172_amd.rotary import _serves
+    x = torch.zeros(3)
+    _serves(x, None)
+    with pytest.raises(ValueError, match="no gradient"):
+        _serves(None, x.clone().requires_grad_(True))
+    with torch.no_grad():
+        _serves(x.clone().requires_grad_(True))
+    with fw.dual_level():
+        _serves(x)
+        for grad in (torch.enable_grad, torch.no_grad):
+            with grad(), pytest.raises(ValueError, match="no gradient"):
+                _serves(fw.make_dual(x, x))
