@@ -96,7 +96,7 @@ def latent_store(cache: LatentCache, latent: torch.Tensor, key_rot: torch.Tensor
     made (no slot twice); the queries' rotary parts q [rows, heads, rot] are turned into q_out in the same launch.
     Returns q_out, None without q."""
     device = _current(cache)
-    _serves(latent, key_rot, q, q_out)
+    _serves(latent, key_rot, q, q_out, freq)
     t = _vectors(latent, "latent", cache.latent, device)
     rows = latent.shape[0]
     if _vectors(key_rot, "key_rot", cache.rot, device) != t or key_rot.shape[0] != rows:
@@ -139,7 +139,7 @@ def latent_attend(q: torch.Tensor, cache: LatentCache, table: torch.Tensor, lens
     """Causal attention of the new tokens q [rows, heads, latent + rot] over their requests' pages, every head over the
     same latents.  ``scale`` is that of the expanded form's keys.  Returns (out [rows, heads, latent], lse [rows, heads] fp32)."""
     device = _current(cache)
-    _serves(q, out)
+    _serves(q, out, lse)
     t = _attend_type(_rows(q, "q", cache.latent + cache.rot, device), "q")
     rows, heads = q.shape[0], q.shape[1]
     n = lens.numel()
@@ -179,7 +179,7 @@ def latent_attend_expanded(q: torch.Tensor, k: torch.Tensor, key_rot: torch.Tens
     and the keys from k_start[i] on, up to the next request's; its last row sees all of its keys.  Returns (out [rows,
     heads, value], lse [rows, heads] fp32)."""
     device = _device()
-    _serves(q, k, key_rot, v, out)
+    _serves(q, k, key_rot, v, out, lse)
     if q.dim() != 3 or k.dim() != 3 or key_rot.dim() != 2 or v.dim() != 3:
         raise ValueError("q, k and v are [rows or keys, heads, dim], key_rot is [keys, rot]")
     nope, rot, value = k.shape[2], key_rot.shape[1], v.shape[2]

@@ -168,7 +168,9 @@ def rotate(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, interle
            magnitude: float = 1.0, inverse: bool = False, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """x [rows, heads, dim] with channels first .. first + 2 freq.numel() turned by positions[row] * freq: pairs
     (i, i + rot / 2), or (2 i, 2 i + 1) where ``interleaved``, times ``magnitude``; by the angles' negatives with
-    ``inverse``.  ``out`` may be x.  Differentiable in x where neither out nor stream is given."""
+    ``inverse``.  ``out`` may be x.  Differentiable in x where neither out nor stream is given, and not in freq."""
+    if _followed(freq):
+        raise ValueError("no gradient goes to the frequencies: detach them")
     if _followed(x) or (out is not None and _followed(out)):
         if out is not None or stream is not None:
             raise ValueError("a rotation that is differentiated takes neither out nor stream")
@@ -211,7 +213,7 @@ def kv_rotate_store(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions:
     """kv_store with the keys turned on the way (their codes are the only rounding), and the step's queries
     q [rows, query heads, dim] turned in the same launch.  No gradient goes through it.  Returns q_out, None without q."""
     device = _current(cache)
-    _serves(k, v, q, q_out)
+    _serves(k, v, q, q_out, freq)
     t = _rows(k, "k", cache.dim, device)
     shape = k.shape
     if _rows(v, "v", cache.dim, device) != t or v.shape != shape or shape[1] != cache.heads:

@@ -90,3 +90,24 @@ def test_tangents(uz):
                 lambda: uz.latent_attend_expanded(h(2, 3, 96), h(2, 3, 64), h(2, 1, 32)[:, 0], d(2, 3, 64), q_start, q_start, 2)):
             with pytest.raises(ValueError, match="no gradient"):
                 call()
+
+
+def test_frequencies_that_are_learned_and_outputs_that_are_followed(uz):
+    """Their gradient would be lost: refused, and taken under no_grad."""
+    g = np.random.default_rng(2)
+    h = lambda *s: rows_of(s, "bf16", g)  # noqa: E731
+    freq, places, slots, q_start = dev(freq_of(32)).requires_grad_(True), ints([0, 1]), torch.tensor([0, 1], device="cuda"), ints([0, 2])
+    pages, cache, lse = uz.KVCache.empty(1, 1, 64, 16), uz.LatentCache.empty(1, 256, 32, 16), torch.zeros(2, 3, device="cuda", requires_grad=True)
+    cache.codes.zero_()
+    cache.exps.fill_(127)
+    calls = [lambda: uz.rotate(h(2, 3, 32), places, freq),
+             lambda: uz.kv_rotate_store(pages, h(2, 1, 64), h(2, 1, 64), places, freq, slots, ints([[0, 2]]), ints([1, 1])),
+             lambda: uz.latent_store(cache, h(2, 1, 256)[:, 0], h(2, 1, 32)[:, 0], places, freq, slots),
+             lambda: uz.latent_attend(h(2, 3, 288), cache, ints([[0]]), ints([2]), q_start, 2, 0.1, lse=lse),
+             lambda: uz.latent_attend_expanded(h(2, 3, 96), h(2, 3, 64), h(2, 1, 32)[:, 0], h(2, 3, 64), q_start, q_start, 2, lse=lse)]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+        with torch.no_grad():
+            call()
+    torch.cuda.synchronize()

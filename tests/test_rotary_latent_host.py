@@ -211,3 +211,12 @@ def test_calls_that_serve_refuse_what_autograd_follows(uz):
         for grad in (torch.enable_grad, torch.no_grad):
             with grad(), pytest.raises(ValueError, match="no gradient"):
                 _serves(fw.make_dual(x, x))
+
+
+def test_rotate_refuses_frequencies_that_are_learned(uz):
+    import torch.autograd.forward_ad as fw
+    x, places, freq = torch.zeros(2, 1, 8), torch.zeros(2, dtype=torch.int32), torch.ones(4)
+    with pytest.raises(ValueError, match="frequencies"):
+        uz.rotate(x, places, freq.clone().requires_grad_(True))
+    with fw.dual_level(), pytest.raises(ValueError, match="frequencies"):
+        uz.rotate(x, places, fw.make_dual(freq, freq))
