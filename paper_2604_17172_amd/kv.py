@@ -191,6 +191,12 @@ def _wrote(*given) -> None:
         _increment(written)
 
 
+def _apart(x, name: str) -> None:
+    """Rows of an output that the caller gave do not share their memory."""
+    if x is not None and x.dim() == 3 and ((x.stride(0) == 0 and x.shape[0] > 1) or (x.stride(1) == 0 and x.shape[1] > 1)):
+        raise ValueError(f"rows or heads of {name} lie on one another")
+
+
 def _current(cache: KVCache) -> int:
     device = _device()
     if cache.index != device:

@@ -14,7 +14,7 @@ import ctypes
 import torch
 
 from . import BF16, EINVAL, FP16, OK, _check, _dev_empty, _lib
-from .kv import _CODES, _TYPES, _device, _handle, _i64, _int, _ints, _need, _on, _rows, _sz, _u32, _vp, _f32, _wrote
+from .kv import _CODES, _TYPES, _device, _handle, _i64, _int, _ints, _need, _on, _rows, _sz, _u32, _vp, _f32, _apart, _wrote
 from .rotary import _queries, _query_args, _serves, _turn, _turn_p
 
 _c = ctypes
@@ -151,6 +151,7 @@ def latent_attend(q: torch.Tensor, cache: LatentCache, table: torch.Tensor, lens
     if not 0 <= max_new < 1 << 32:
         raise ValueError("max_new is not negative")
     given = out, lse
+    _apart(out, "out")
     if out is None or lse is None or ws is None:
         with _on(stream):
             out = torch.empty(rows, heads, cache.latent, dtype=q.dtype, device=q.device) if out is None else out
@@ -196,6 +197,7 @@ def latent_attend_expanded(q: torch.Tensor, k: torch.Tensor, key_rot: torch.Tens
     if not 0 <= max_new < 1 << 32:
         raise ValueError("max_new is not negative")
     given = out, lse
+    _apart(out, "out")
     if out is None or lse is None:
         with _on(stream):
             out = torch.empty(rows, heads, value, dtype=q.dtype, device=q.device) if out is None else out

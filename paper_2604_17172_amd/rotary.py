@@ -15,7 +15,7 @@ import torch
 import torch.autograd.forward_ad as _forward
 
 from . import OK, _check, _lib
-from .kv import KVCache, _TYPES, _cache_p, _current, _device, _handle, _i64, _int, _ints, _on, _rows, _u32, _vp, _wrote
+from .kv import KVCache, _TYPES, _cache_p, _current, _device, _handle, _i64, _int, _ints, _on, _rows, _u32, _vp, _apart, _wrote
 
 _c = ctypes
 
@@ -121,6 +121,7 @@ def _rotate(x, positions, freq, interleaved, first, magnitude, inverse, out, str
     if first + turn.rot > dim:
         raise ValueError("the rotary part lies within dim")
     given = out
+    _apart(out, "out")
     if out is None:
         with _on(stream):
             out = torch.empty(rows, heads, dim, dtype=x.dtype, device=x.device)
@@ -192,6 +193,7 @@ def _queries(q, q_out, rows: int, dim: int, device: int, kind: int, stream):
         return None, None
     if _rows(q, "q", dim, device) != kind or q.shape[0] != rows:
         raise ValueError("q has the rows and the type of what is stored")
+    _apart(q_out, "q_out")
     if q_out is None:
         with _on(stream):
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)

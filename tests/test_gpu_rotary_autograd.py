@@ -111,3 +111,23 @@ def test_frequencies_that_are_learned_and_outputs_that_are_followed(uz):
         with torch.no_grad():
             call()
     torch.cuda.synchronize()
+
+
+def test_outputs_whose_rows_share_memory_are_refused(uz):
+    """One rotary key for all heads, turned where it is, would be turned once for each."""
+    g = np.random.default_rng(4)
+    h = lambda *s: rows_of(s, "bf16", g)  # noqa: E731
+    freq, places, slots, q_start = dev(freq_of(32)), ints([0, 1]), torch.tensor([0, 1], device="cuda"), ints([0, 2])
+    pages, cache = uz.KVCache.empty(1, 1, 64, 16), uz.LatentCache.empty(1, 256, 32, 16)
+    key = h(2, 1, 32).expand(2, 3, 32)
+    calls = [lambda: uz.rotate(key, places, freq, out=key),
+             lambda: uz.kv_rotate_store(pages, h(2, 1, 64), h(2, 1, 64), places, freq, slots, ints([[0, 2]]), ints([1, 1]), q=h(2, 3, 64),
+                                        q_out=h(1, 3, 64).expand(2, 3, 64)),
+             lambda: uz.latent_store(cache, h(2, 1, 256)[:, 0], h(2, 1, 32)[:, 0], places, freq, slots, q=h(2, 3, 32), q_out=key),
+             lambda: uz.latent_attend(h(2, 3, 288), cache, ints([[0]]), ints([2]), q_start, 2, 0.1, out=h(2, 1, 256).expand(2, 3, 256)),
+             lambda: uz.latent_attend_expanded(h(2, 3, 96), h(2, 3, 64), h(2, 1, 32)[:, 0], h(2, 3, 64), q_start, q_start, 2, out=h(1, 3, 64).expand(2, 3, 64))]
+    for call in calls:
+        with pytest.raises(ValueError, match="lie on one another"):
+            call()
+    turned = uz.rotate(key, places, freq)                                 # read, they may
+    assert torch.equal(turned, uz.rotate(key.contiguous(), places, freq))

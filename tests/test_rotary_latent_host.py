@@ -220,3 +220,13 @@ def test_rotate_refuses_frequencies_that_are_learned(uz):
         uz.rotate(x, places, freq.clone().requires_grad_(True))
     with fw.dual_level(), pytest.raises(ValueError, match="frequencies"):
         uz.rotate(x, places, fw.make_dual(freq, freq))
+
+
+def test_outputs_whose_rows_share_memory(uz):
+    from paper_2604_17172_amd.kv import _apart
+    x = torch.zeros(3, 2, 8)
+    for good in (None, x, x[:, :1], x[:1].expand(1, 2, 8), torch.zeros(3, 1, 8).expand(3, 1, 8), x[:0], x.transpose(0, 1)):
+        _apart(good, "out")
+    for bad in (x[:1].expand(3, 2, 8), x[:, :1].expand(3, 2, 8)):
+        with pytest.raises(ValueError, match="lie on one another"):
+            _apart(bad, "out")
