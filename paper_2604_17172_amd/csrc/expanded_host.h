@@ -17,11 +17,12 @@ struct ExpandedCall {
   hipStream_t stream;
 };
 
-// Whether 64 rows' sums, queries, scores of two tiles and weights leave a SIMD's registers for two waves: 128 rows then go
-// to eight waves, each pair a quarter of the tokens.  64 + 32 and 64 channels, fp16, 7 ragged requests of 6 heads: 38 us, by four
-// waves 43; 2048 tokens of 16 heads 32 and 36; 4 x 1024 39 and 40; 8 x 512 of 8 heads 18 and 17.  (64 + 64 and 64, where
-// registers spill: 35 and 39, 43 and 43, 21 and 18.)
-constexpr bool expanded_by_eight(uint32_t nope, uint32_t rot, uint32_t value) { return 2 * (value / 2 + (nope + rot) / 4 + 40) <= 200; }
+// Whether 128 rows go to eight waves, each pair a quarter of the tokens.  The narrowest kernel alone: two of its waves to a SIMD have
+// registers for 64 rows' sums, queries, scores of two tiles and weights; 8 words that a block's beginning and end need are in memory
+// meanwhile.  64 + 32 and 64 channels, fp16, 7 ragged requests of 6 heads: 38 us, by four
+// waves 43; 2048 tokens of 16 heads 32 and 36; 4 x 1024 39 and 40; 8 x 512 of 8 heads 18 and 17.  (64 + 64 and 64, where the
+// loop's registers spill: 35 and 39, 43 and 43, 21 and 18.)
+constexpr bool expanded_by_eight(uint32_t nope, uint32_t rot, uint32_t value) { return nope == 64 && rot == 32 && value == 64; }
 
 template <int DN>
 uzip_status launch_expanded(const ExpandedCall &c);

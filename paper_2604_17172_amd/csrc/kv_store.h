@@ -49,17 +49,6 @@ struct Eight {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
   }
-  __device__ __forceinline__ void put(const float *x) {
-    Value v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (Value)x[j];
-    __builtin_memcpy(w, v, sizeof(w));
-  }
-  // to multiples of 16 bytes
-  __device__ __forceinline__ void store(Value *x) const {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(Value) / 2; ++i) ((u32x4 *)x)[i] = w[i];
-  }
 };
 
 // The codes of places 0 .. off - 1 again, where the page's scale grew.
