@@ -28,23 +28,21 @@ struct CosSin {
 
 // The angle is taken in 64 bits: at position 2^20 a product in 32 bits is off by up to 2^-4.
 // What is left of it after whole quarter turns, x and what 32 bits of x leave, goes to the two Taylor series up to
-// x^10, |x| <= pi / 4: the first term left out is below 2e-9, a sine is off by 1.5 half steps at most, a cosine by 2.3.
+// x^10, |x| <= pi / 4: the first term left out is below 2e-9, a sine is off by 1.5 half steps at most, a cosine by 1.25.
 __device__ __forceinline__ CosSin turn_of(const Turn &t, int32_t p, uint32_t pair) {
   const double quarters = (double)p * (double)t.freq[pair] * 0.63661977236758134308;  // 2 / pi
-  const double rest = quarters - 4.0 * __builtin_rint(0.25 * quarters);               // -2 .. 2
-  const double n = __builtin_rint(rest);
-  const double angle = (rest - n) * 1.57079632679489661923;
-  const float x = (float)angle, low = (float)(angle - (double)x), z = x * x;
-  const int q = (int)n;
+  const double n = __builtin_rint(quarters), angle = (quarters - n) * 1.57079632679489661923;
+  const uint32_t q = (uint32_t)__builtin_bit_cast(uint64_t, n + 6755399441055744.0);  // n's last bits: 1.5 * 2^52 has a step of 1
+  const float x = (float)angle, low = (float)(angle - (double)x), z = x * x, z_low = __builtin_fmaf(x, x, -z);
+  const float h = __builtin_fmaf(z, -0.5f, 1.0f), h_low = __builtin_fmaf(z, -0.5f, 1.0f - h);  // 1 - z / 2 and what it leaves
   float s = __builtin_fmaf(z, 1.0f / 362880, -1.0f / 5040);
   s = __builtin_fmaf(z, s, 1.0f / 120);
   s = __builtin_fmaf(z, s, -1.0f / 6);
-  s = x + __builtin_fmaf(x * z, s, low * __builtin_fmaf(z, -0.5f, 1.0f));
+  s = x + __builtin_fmaf(x * z, s, __builtin_fmaf(x * z_low, -1.0f / 6, low * h));
   float c = __builtin_fmaf(z, -1.0f / 3628800, 1.0f / 40320);
   c = __builtin_fmaf(z, c, -1.0f / 720);
   c = __builtin_fmaf(z, c, 1.0f / 24);
-  c = __builtin_fmaf(z, c, -0.5f);
-  c = 1.0f + __builtin_fmaf(z, c, -(x * low));
+  c = h + __builtin_fmaf(z * z, c, h_low - __builtin_fmaf(0.5f, z_low, x * low));
   const float cc = q & 1 ? s : c, ss = q & 1 ? c : s;
   // quarter turns: (c, s), (-s, c), (-c, -s), (s, -c)
   const float m = t.magnitude;

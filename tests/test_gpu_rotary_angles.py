@@ -35,3 +35,18 @@ def test_sines_and_cosines(uz, interleaved):
         off = np.abs(value - want) - 2.0 ** -50 * np.abs(angle)
         assert (off[by_sine] <= 1.6 * 2.0 ** -25).all(), off[by_sine].max() * 2.0 ** 25
         assert (off[~by_sine] <= 2.45 * 2.0 ** -25).all(), off[~by_sine].max() * 2.0 ** 25
+
+
+def test_cosines_within_a_step(uz):
+    """1 - x x / 2 with what its product and its sum leave, and a tail |u| < 0.016: the last sum's rounding (1), the tail's (0.2), the
+    series (0.01)."""
+    places = np.arange(-(1 << 18), 1 << 18)
+    freq = np.array([2.0 ** -12 * np.pi / 8], np.float32)               
+    x = torch.zeros(len(places), 1, 2, device="cuda")
+    x[..., 0] = 1
+    got = np_of(uz.rotate(x, ints(places), dev(freq)))[:, 0]
+    angle = places.astype(np.float64) * freq.astype(np.float64)
+    odd = np.rint(angle / (np.pi / 2)).astype(np.int64) & 1
+    value, want = np.where(odd, got[:, 1], got[:, 0]), np.where(odd, np.sin(angle), np.cos(angle))
+    off = np.abs(value - want) - 2.0 ** -50 * np.abs(angle)
+    assert (off <= 1.25 * 2.0 ** -25).all(), off.max() * 2.0 ** 25
