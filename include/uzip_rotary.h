@@ -23,7 +23,7 @@ typedef struct {
   uint32_t first;           /* the channel where it begins */
   uint32_t interleaved;     /* 0: pairs (i, i + rot / 2); 1: pairs (2 i, 2 i + 1) */
   uint32_t inverse;         /* 1: the angle's sign changed, which is also the gradient */
-  float magnitude;          /* m, on the rotary part alone */
+  double magnitude;         /* m, on the rotary part alone; finite in 32 bits */
 } uzip_turn;
 
 /* The place of each row in its request, from what uzip_kv_plan leaves: row j of request i

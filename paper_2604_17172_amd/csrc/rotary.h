@@ -19,7 +19,7 @@ struct Turn {
   uint32_t first;      // channel where the rotary part begins
   bool interleaved;    // pairs (2 i, 2 i + 1), else (i, i + half)
   bool even;           // half and first are multiples of 8: no eight channels hold two kinds
-  float magnitude, sign;
+  float m, m_low, sign;  // the magnitude and what 32 bits of it leave
 };
 
 struct CosSin {
@@ -38,15 +38,16 @@ __device__ __forceinline__ CosSin turn_of(const Turn &t, int32_t p, uint32_t pai
   float s = __builtin_fmaf(z, 1.0f / 362880, -1.0f / 5040);
   s = __builtin_fmaf(z, s, 1.0f / 120);
   s = __builtin_fmaf(z, s, -1.0f / 6);
-  s = x + __builtin_fmaf(x * z, s, __builtin_fmaf(x * z_low, -1.0f / 6, low * h));
+  s = __builtin_fmaf(x * z, s, __builtin_fmaf(x * z_low, -1.0f / 6, low * h));  // x + s
   float c = __builtin_fmaf(z, -1.0f / 3628800, 1.0f / 40320);
   c = __builtin_fmaf(z, c, -1.0f / 720);
   c = __builtin_fmaf(z, c, 1.0f / 24);
-  c = h + __builtin_fmaf(z * z, c, h_low - __builtin_fmaf(0.5f, z_low, x * low));
+  c = __builtin_fmaf(z * z, c, h_low - __builtin_fmaf(0.5f, z_low, x * low));  // h + c
+  s = __builtin_fmaf(t.m, x, __builtin_fmaf(t.m, s, t.m_low * x));
+  c = __builtin_fmaf(t.m, h, __builtin_fmaf(t.m, c, t.m_low * h));
   const float cc = q & 1 ? s : c, ss = q & 1 ? c : s;
   // quarter turns: (c, s), (-s, c), (-c, -s), (s, -c)
-  const float m = t.magnitude;
-  return {((q + 1) & 2 ? -cc : cc) * m, (q & 2 ? -ss : ss) * m * t.sign};
+  return {(q + 1) & 2 ? -cc : cc, (q & 2 ? -ss : ss) * t.sign};
 }
 
 __device__ __forceinline__ void turn_pair(const CosSin &r, float &a, float &b) {
@@ -205,13 +206,14 @@ __device__ __forceinline__ void turn_rows(const TurnRows &a, const Turn &t, uint
 // ------------------------------------------------------------------ host
 inline bool valid_turn(const uzip_turn *t) {
   return t && t->rot >= 2 && t->rot <= 1024 && t->rot % 2 == 0 && t->first <= 1024 && t->interleaved <= 1 && t->inverse <= 1 &&
-         t->magnitude - t->magnitude == 0;
+         (float)t->magnitude - (float)t->magnitude == 0;
 }
 inline bool valid_places(const uzip_turn *t) { return t->positions && t->freq && aligned(t->positions, 4) && aligned(t->freq, 4); }
 
 inline Turn turn_args(const uzip_turn *t) {
   const uint32_t half = t->rot / 2;
-  return {t->positions, t->freq, half, t->first, t->interleaved != 0, half % 8 == 0 && t->first % 8 == 0, t->magnitude, t->inverse ? -1.0f : 1.0f};
+  return {t->positions, t->freq, half, t->first, t->interleaved != 0, half % 8 == 0 && t->first % 8 == 0, (float)t->magnitude,
+          (float)(t->magnitude - (double)(float)t->magnitude), t->inverse ? -1.0f : 1.0f};
 }
 
 // What a launch over rows of heads needs; false where they cannot be.

@@ -22,7 +22,7 @@ _c = ctypes
 
 class uzip_turn(_c.Structure):
     _fields_ = [("positions", _vp), ("freq", _vp), ("rot", _u32), ("first", _u32), ("interleaved", _u32), ("inverse", _u32),
-                ("magnitude", _c.c_float)]
+                ("magnitude", _c.c_double)]
 
 
 _turn_p = _c.POINTER(uzip_turn)

@@ -50,3 +50,25 @@ def test_cosines_within_a_step(uz):
     value, want = np.where(odd, got[:, 1], got[:, 0]), np.where(odd, np.sin(angle), np.cos(angle))
     off = np.abs(value - want) - 2.0 ** -50 * np.abs(angle)
     assert (off <= 1.25 * 2.0 ** -25).all(), off.max() * 2.0 ** 25
+
+
+@pytest.mark.parametrize("magnitude", [1.2, 0.1 * np.log(7) + 1, 1 / 3, -1.1])
+def test_magnitudes_that_32_bits_do_not_hold(uz, magnitude):
+    """m (1, 0) turned: beside the functions' own errors, at most 1.6 and 1.25 half steps of 1/2 to 1 times m, the product's rounding."""
+    places, freq = np.arange(40000), np.array([0.37, 1.0, 0.001], np.float32)
+    x = torch.zeros(len(places), 1, 6, device="cuda")
+    x[..., :3] = 1
+    got = np_of(uz.rotate(x, ints(places), dev(freq), magnitude=magnitude))[:, 0]
+    angle = places[:, None].astype(np.float64) * freq
+    want = magnitude * np.concatenate([np.cos(angle), np.sin(angle)], axis=1)
+    tail = np.where(np.abs(want) <= abs(magnitude) * 0.7072, 0.6, 0.25)   # what a function is off by beside its last rounding, which is the product's
+    step = 2.0 ** (np.floor(np.log2(np.abs(want) + 2.0 ** -60)) - 23)
+    tol = step / 2 + (tail * 2.0 ** -25 + 2.0 ** -50 * np.tile(angle, 2)) * abs(magnitude) * (1 + 2.0 ** -20)
+    assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
+
+
+def test_turns_are_refused_by_their_magnitude_in_32_bits(uz):
+    x, places, freq = torch.zeros(1, 1, 2, device="cuda"), ints([0]), dev(np.ones(1, np.float32))
+    for magnitude in (1e39, -1e39, float("inf"), float("nan")):
+        with pytest.raises(uz.UzipError):
+            uz.rotate(x, places, freq, magnitude=magnitude)
