@@ -377,12 +377,13 @@ __device__ __forceinline__ uint32_t not_numbers(uint32_t w) {
 // its registers, and makes their weights.  Two add: each takes half of the channels, with 32 x DC / 2 sums
 // in its registers, and asks for the tiles.  Scoring and adding a tile are a round apart, so that a compute unit's
 // matrix units have the products of the one beside the conversions and exponentials of the other; a wave that did both would
-// need all 512 registers, and nothing would run beside it (32 requests of 1000 to 16383 tokens, 128 heads: 126 us, now 91).
+// need all 512 registers, and nothing would run beside it (32 requests of 1000 to 16383 tokens, 128 heads: 126 us, then 91; 94 with
+// weights that keep their bits).
 // Between the two barriers of a round the scores' maxima are exchanged.
 // A round takes 1.7 us with 32 rows of 512, 1.9 with 64, 1.6 with 64 of 256 in fp16; of 512 with 64 rows that is 3800
 // cycles, of which the matrix units work 2200: the rest is the wait of one kind of waves for the other, and the
 // loads, which one wave's instructions ask for a kilobyte at a time.  64 requests of up to 8190 tokens of 512 + 64, 16
-// heads: 41 us, 3.7 TB/s; 128 heads as above: 91 us, 850 TFLOP/s.
+// heads: 43 us, 3.6 TB/s; 128 heads as above: 94 us, 825 TFLOP/s.
 template <int T, int CODE, int DC, int RG>
 struct Latent {
   static constexpr int kRows = 32 * RG, kThreads = 256 * RG, kBlocks = DC / 64, kSteps = DC / 32;

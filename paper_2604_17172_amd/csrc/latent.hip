@@ -11,7 +11,7 @@ namespace {
 // ------------------------------------------------------------------ store
 // A wave for each row: its latent (four or eight channels a lane), its rotary key (a pair to each of
 // the first lanes), the largest of each by exchanges, the codes.  No row waits for another, since scales
-// are a token's own.  16384 rows of 512 + 64 in bf16, 28 MB: 9.8 us, 2.9 TB/s; a wave's chain of loads, maxima and
+// are a token's own.  16384 rows of 512 + 64 in bf16, 28 MB: 9.6 us, 2.9 TB/s; a wave's chain of loads, maxima and
 // stores is the bound, not the bytes (5.6 us).
 struct LatentStoreArgs {
   uint8_t *codes, *exps;

@@ -16,8 +16,10 @@ static uzip_status launch(LatentCall &c) {
   a.by_heads = FastDiv::of(a.heads);
   a.growth = (double)L::kRows / ((double)kTile * a.heads);
   // What a block's beginning and end cost a workgroup, in tiles.  Counted as 1, workgroups with the end of one block and the
-  // beginning of the next were 30 % later than others.  Of 512: 6 (64 requests of up to 8190 tokens, 16 heads: 41 us, with 4
-  // 44, with 1 50); of 256: 4 (16 requests' pieces: 71 us, with 6 74, with 1 74).
+  // beginning of the next were 30 % later than others.  A call, us with 1, 4, 6, 9 of 64 requests of 1000 to 8190 tokens: of 512 in bf16, 16
+  // heads 53, 50, 48, 49, 128 heads 108, 101, 98, 98; in fp16 56, 53, 52, 53 and 125, 116, 113, 114; of 256 in bf16 41, 38, 38, 38 and 77,
+  // 72, 71, 72, in fp16 43, 40, 41, 42 and 86, 79, 80, 81.  16 requests of 500 to 4000, 32 heads, few tiles to a workgroup: of 512
+  // 29, 29, 32, 39, of 256 23, 22, 25, 30.  Two pieces behind 5000 and 8000, 12 heads: of 512 93, 91, 90, 91, of 256 68, 66, 66, 67.
   a.begin = LATENT_DIM == 512 ? 6 : 4;
   // At most how much work there is: blocks, and the tiles of each.
   const uint64_t rows = (uint64_t)a.n_rows * a.heads;

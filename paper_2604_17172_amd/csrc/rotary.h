@@ -143,7 +143,7 @@ constexpr uint32_t kTurnTable = 1024;  // turns that a workgroup holds, at most:
 // One workgroup's rows.  The turns of a row are the same for all its heads: they are
 // worked out once, into LDS, while the first values are on their way.  Bound by the rows' bytes: 16384 rows of
 // 32 heads of 128 in bf16, 268 MB in 44 us, 6.1 TB/s.  Units of four pairs keep wide loads where the rotary part
-// is no multiple of 8: 4099 rows of 11 heads of 104 in fp32, 40 of them turned, 37.5 MB in 8.3 us (pair by
+// is no multiple of 8: 4099 rows of 11 heads of 104 in fp32, 40 of them turned, 37.5 MB in 8.5 us (pair by
 // pair: 34.5 us).
 template <int T, int W>
 __device__ __forceinline__ void turn_units(const TurnRows &a, const Turn &t, uint32_t block, CosSin *table) {

@@ -201,7 +201,7 @@ __device__ __forceinline__ void store_turned_one(const StoreArgs &a, const Turn 
 
 // Workgroups: for each run, head and of keys and values one (or a wave, FEW); the rest turn queries.  Every
 // function is inlined: as calls they took 199 registers, and 16384 tokens of 32 and 8 heads of 128 in bf16
-// 202 us.  Now their 369 MB take 86 us, 4.3 TB/s, with 95 registers, which five waves a SIMD leave each; with 100, and so four
+// 202 us.  Now their 369 MB take 88 us, 4.2 TB/s, with 95 registers, which five waves a SIMD leave each; with 100, and so four
 // waves, the call took 92.5 us instead of 89.3, and with the pairs' turns one half after the other, in 87 registers, 130.
 template <int T, int CODE, bool FEW>
 __global__ __launch_bounds__(256, FEW ? 4 : 5) void rotate_store_kernel(StoreArgs a, TurnRows q, Turn t, uint32_t max_runs, uint32_t head_blocks, bool turn_vec) {
