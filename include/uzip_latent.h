@@ -63,10 +63,10 @@ size_t uzip_latent_attend_workspace(uint32_t latent, uint32_t n_rows, uint32_t n
  * infinity makes the rows that see it NaN, and no others.  A rotary key that holds one counts by its
  * score: minus infinity as no token, another one that is not finite makes its row NaN.
  * dtype is UZIP_BF16 or UZIP_FP16.  Scores and sums are held in 32 bits.  A weight enters the second
- * product with at least 8 bits for bf16, 12 for fp16, or off by at most 2^-21 (2^-25) of the
- * largest weight of its 64 tokens (those whose places are equal but for the last six
- * bits).  That product is one of 8-bit matrix instructions: of eight terms side by side, what lies 2^-13 below the
- * largest is dropped.
+ * product, times its latent's scale, with at least 8 bits for bf16, 12 for fp16, or off by at
+ * most 2^-21 (2^-25) of the largest such of its 64 tokens (those whose places are equal but for
+ * the last six bits).  That product is one of 8-bit matrix instructions: of eight terms side by
+ * side, what lies 2^-13 below the largest is dropped.
  *   max_new:  the most new tokens of a request: it chooses kernels, a wrong value costs
  *             time and the last bits may differ.
  * n_rows * n_heads <= UZIP_KV_MAX_ROW_HEADS; n_heads <= 1024; n_reqs <= UZIP_KV_MAX_REQUESTS.

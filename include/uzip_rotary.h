@@ -34,7 +34,8 @@ uzip_status uzip_kv_positions(const int32_t *d_lens, const int32_t *d_q_start, u
                               int32_t *d_positions, hipStream_t stream);
 
 /* out[row][head] = x[row][head] turned; channels outside the rotary part are copied.
- * head_dim is any number up to 1024 with first + rot <= head_dim.  d_out with d_x's
+ * head_dim is any number up to 1024 with first + rot <= head_dim, n_heads up to 65535, n_rows *
+ * n_heads up to UZIP_KV_MAX_ROW_HEADS.  d_out with d_x's
  * strides may be d_x; otherwise no value of the one lies on a value of the other.
  * Errors: EINVAL, EHIP, EUNSUPPORTED. */
 uzip_status uzip_rotate(uzip_dtype dtype, const void *d_x, int64_t x_row, int64_t x_head, uint32_t n_rows,
